@@ -315,6 +315,46 @@ int spark_mha_strided_bwd(const void* Q, const void* K, const void* V, const voi
                           spark_dtype_t dtype, void* stream);
 
 /*
+ * Norm of every head's query and key vector and its rotation by position, in one pass: what a decoder does to its
+ * projected queries and keys before the attention.  For a row x of Q or K (its head's d elements), all in fp32:
+ *   n = x / sqrt(mean(x^2) + eps),   y = n * w,   out = R y, rounded once,
+ * where R turns the pairs of the first rd elements by the angles of the row's position p: with c = cos[p][i],
+ * s = sin[p][i], pair i = (y[i], y[i + rd/2]), or (y[2i], y[2i+1]) if interleaved, becomes (a c - b s, b c + a s).
+ *   Q, Qr     : in, out, device, [B,H,N,d] dtype;   K, Kr : [B,Hkv,N,d] dtype.  Any strides as below; the result may be
+ *               written in place (Qr = Q with Q's strides), or straight into the rows of a cache.
+ *   wq, wk    : in, device, [d], fp32 (w_fp32 != 0) or dtype; NULL: ones
+ *   cos, sin  : in, device, [table, rd/2] fp32, contiguous, 16-byte aligned.  NULL if rd = 0.
+ *   positions : in, device, [B,N] int32: each token's row of the tables; NULL: token n has position n (N <= table).
+ *               A negative position marks padding: the token's results are zeros, and it adds to no gradient.  A
+ *               position behind the table (a mistake that the host cannot see) gives NaN; nothing is read there.
+ * Supported: d a multiple of 8 in 8..128; rd a multiple of 8 in 0..d; H, Hkv <= 32768; B*N < 2^31 - 65536; eps finite
+ * and > 0.  Strides as in spark_mha_strided_fwd, but of any size (64-bit offsets), and the stride of an index with one
+ * value does not matter.
+ */
+int spark_qk_norm_rope_fwd(const void* Q, const void* K, const void* wq, const void* wk, const float* cos, const float* sin,
+                           const int* positions, void* Qr, void* Kr, const spark_strides_t* sQ, const spark_strides_t* sK,
+                           const spark_strides_t* sQr, const spark_strides_t* sKr, int B, int N, int H, int Hkv, int d,
+                           int rd, int table, float eps, int interleaved, int w_fp32, spark_dtype_t dtype, void* stream);
+
+/*
+ * Its backward.  With dout the gradient of a result row: dy = R^T dout, t = dy * w, dx = r (t - n mean(t n)) for
+ * r = 1 / sqrt(mean(x^2) + eps); dw = sum of dy * n over all rows (the sums are fp32, in a fixed order).
+ *   Q, K, wq, wk, cos, sin, positions : in, as given to the forward (Q, K before the forward: not to be overwritten by it)
+ *   dQr, dKr  : in,  device, [B,H,N,d], [B,Hkv,N,d] dtype;   dQ, dK : out, the same shapes (dQ = dQr in place is allowed)
+ *   dwq, dwk  : out, device, [d] fp32, whatever the weights' type; written for wq, wk = NULL too
+ *   workspace : device scratch of at least spark_qk_norm_rope_bwd_workspace_bytes(...) bytes, 16-byte aligned.  Its size
+ *               is at most 2048 + H + Hkv rows of d floats.  0 for invalid shapes.
+ */
+size_t spark_qk_norm_rope_bwd_workspace_bytes(int B, int N, int H, int Hkv, int d, int rd, spark_dtype_t dtype);
+
+int spark_qk_norm_rope_bwd(const void* Q, const void* K, const void* wq, const void* wk, const float* cos, const float* sin,
+                           const int* positions, const void* dQr, const void* dKr, void* dQ, void* dK, float* dwq,
+                           float* dwk, const spark_strides_t* sQ, const spark_strides_t* sK, const spark_strides_t* sdQr,
+                           const spark_strides_t* sdKr, const spark_strides_t* sdQ, const spark_strides_t* sdK,
+                           void* workspace, size_t workspace_bytes, int B, int N, int H, int Hkv, int d, int rd, int table,
+                           float eps, int interleaved, int w_fp32, spark_dtype_t dtype, void* stream);
+
+/*
  * Hardware self-check of the register layouts the kernels are written against (wave64
  * 32x32x16 MFMA operands and accumulators, packed accumulator registers reused as the operand
  * of a second MFMA -- the register form of the paper's Sec. 3.2.2 layout transform -- and the

@@ -1,6 +1,7 @@
 """Fused multi-head attention (forward + backward) for MI355X, behind a C ABI.
 
-``binding`` marshals torch device tensors into ``libspark_mha.so``;
+``binding`` marshals torch device tensors into ``libspark_mha.so``, ``decoder`` those of the operators around a
+decoder's attention;
 ``synth`` generates the seeded synthetic workloads; ``build`` compiles the library.
 """
 from .binding import (  # noqa: F401
@@ -27,4 +28,9 @@ from .binding import (  # noqa: F401
     spark_mha_strided_bwd,
     spark_mha_strided_fwd,
     status_str,
+)
+from .decoder import (  # noqa: F401
+    spark_qk_norm_rope_bwd,
+    spark_qk_norm_rope_bwd_workspace_bytes,
+    spark_qk_norm_rope_fwd,
 )

@@ -5,11 +5,13 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspark_mha.so")
-SOURCES = [os.path.join(CSRC, "spark_mha.hip")]
+SOURCES = [os.path.join(CSRC, "spark_mha.hip"), os.path.join(CSRC, "decoder_ops.hip")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # a rule for the test machines: never let the compiler form packed-fp32 instructions
@@ -18,16 +20,32 @@ HIPCC_FLAGS = [
 ]
 
 
-def build_library(verbose: bool = False) -> str:
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [hipcc] + HIPCC_FLAGS + SOURCES + ["-o", tmp]
+def _hipcc(args):
+    """Run hipcc; its output, without the host pass's remark about the device feature."""
+    cmd = [os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")] + args
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     out = "\n".join(l for l in res.stdout.splitlines() if "not a recognized feature" not in l)
     if res.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + out)
-    if verbose and out.strip():
-        print(out)
+    return out
+
+
+def _each_source(flags, suffix, folder):
+    """Compile every source by itself, all at once; (files, outputs of the compiler)."""
+    files = [os.path.join(folder, os.path.basename(s) + suffix) for s in SOURCES]
+    with ThreadPoolExecutor(len(SOURCES)) as pool:
+        return files, list(pool.map(lambda sf: _hipcc(flags + [sf[0], "-o", sf[1]]), zip(SOURCES, files)))
+
+
+def build_library(verbose: bool = False) -> str:
+    tmp = LIB + ".tmp.%d" % os.getpid()
+    with tempfile.TemporaryDirectory() as folder:
+        files, outs = _each_source([f for f in HIPCC_FLAGS if f != "-shared"] + ["-c"], ".o", folder)
+        outs.append(_hipcc(["--offload-arch=gfx950", "-shared"] + files + ["-o", tmp]))
+    if verbose:
+        for out in outs:
+            if out.strip():
+                print(out)
     os.replace(tmp, LIB)
     return LIB
 
@@ -76,16 +94,10 @@ def build_mix_floor_bench() -> str:
 def device_assembly():
     """(assembly text, compiler remarks) of the library's device code; nothing is written next to
     the sources."""
-    import tempfile
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in HIPCC_FLAGS if f not in ("-fPIC", "-shared")]
     with tempfile.TemporaryDirectory() as tmp:
-        cmd = [hipcc] + flags + ["--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage"] + SOURCES
-        res = subprocess.run(cmd + ["-o", os.path.join(tmp, "out.s")], stdout=subprocess.PIPE,
-                             stderr=subprocess.STDOUT, text=True)
-        if res.returncode != 0:
-            raise RuntimeError("hipcc failed:\n" + res.stdout)
-        return open(os.path.join(tmp, "out.s")).read(), res.stdout
+        files, remarks = _each_source(flags + ["--cuda-device-only", "-S", "-Rpass-analysis=kernel-resource-usage"], ".s", tmp)
+        return "\n".join(open(f).read() for f in files), "\n".join(remarks)
 
 
 def unguarded_lds_loads(asm: str):

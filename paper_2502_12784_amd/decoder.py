@@ -1,0 +1,128 @@
+"""The operators around a decoder's attention: norm and rotation of queries and keys, attention behind a shared prefix.
+
+Argument marshalling only, as in ``binding``: the work is done by the HIP kernels of ``libspark_mha.so``.
+"""
+from __future__ import annotations
+
+from . import binding
+from .binding import Strides, _check, _dtype_code, _stream_ptr, load_library
+
+
+def _same_device(*tensors):
+    """All tensors given (None: not given) on the current device; the kernels run there."""
+    import torch
+    for name, t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("%s is on %s, not on the current device %d" % (name, t.device, torch.cuda.current_device()))
+
+
+def _rows(t, shape, dtype, name):
+    """Check a [B,H,N,d] view whose last dimension is contiguous; return its spark_strides_t."""
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise ValueError("%s must be a %s view of shape %s with contiguous last dimension"
+                         % (name, dtype, tuple(shape)))
+    return Strides(t.stride(0), t.stride(1), t.stride(2))
+
+
+def _ints(t, shape, name):
+    """An optional contiguous int32 tensor; its address."""
+    import torch
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
+def _scratch(workspace, need, like):
+    import torch
+    if workspace is None:
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=like.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _qk_problem(Q, K, wq, wk, cos, sin, positions, eps, interleaved):
+    """(tensors' addresses, sizes, flags) shared by both directions of spark_qk_norm_rope."""
+    import torch
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("Q must be [B,H,N,d] and K [B,Hkv,N,d]")
+    B, H, N, d = Q.shape
+    code = _dtype_code(Q)
+    _same_device(("Q", Q), ("K", K), ("wq", wq), ("wk", wk), ("cos", cos), ("sin", sin), ("positions", positions))
+    given = [w for w in (wq, wk) if w is not None]
+    for w in given:
+        if tuple(w.shape) != (d,) or w.dtype not in (torch.float32, Q.dtype) or not w.is_contiguous():
+            raise ValueError("wq and wk must be contiguous [%d] tensors of float32 or %s" % (d, Q.dtype))
+    if len(given) == 2 and wq.dtype != wk.dtype:
+        raise ValueError("wq and wk must have the same type")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin are given together")
+    table = rd = 0
+    if cos is not None:
+        if cos.dim() != 2:
+            raise ValueError("cos and sin must be [positions, rd / 2]")
+        table, rd = cos.shape[0], 2 * cos.shape[1]
+        for t, n in ((cos, "cos"), (sin, "sin")):
+            if tuple(t.shape) != tuple(cos.shape) or t.dtype != torch.float32 or not t.is_contiguous():
+                raise ValueError("%s must be a contiguous float32 tensor of shape %s" % (n, tuple(cos.shape)))
+    at = _ints(positions, (B, N), "positions")
+    address = [None if t is None else t.data_ptr() for t in (wq, wk, cos, sin)] + [at]
+    fp32 = int(bool(given) and given[0].dtype == torch.float32)
+    sizes = (B, N, H, K.shape[1], d, rd, table, float(eps), int(bool(interleaved)), fp32, code)
+    return address, sizes
+
+
+def spark_qk_norm_rope_fwd(Q, K, wq, wk, cos, sin, positions=None, eps: float = 1e-6, interleaved: bool = False, Qr=None,
+                           Kr=None):
+    """Qr, Kr: every head's row of Q [B,H,N,d] and K [B,Hkv,N,d] divided by its root mean square, scaled by wq, wk ([d],
+    fp32 or the tensors' type; None: not scaled) and its first 2 * cos.shape[1] elements rotated by its position's row of
+    cos, sin ([positions, rd / 2] fp32; None: no rotation).  positions: [B,N] int32 (None: 0 ... N-1); a negative one marks
+    padding, whose results are zeros.  Any strides; Qr and Kr may be given, as Q and K themselves or as rows of a cache."""
+    import torch
+    lib = load_library()
+    address, sizes = _qk_problem(Q, K, wq, wk, cos, sin, positions, eps, interleaved)
+    B, N, H, Hkv, d = sizes[:5]
+    Qr = torch.empty_like(Q) if Qr is None else Qr
+    Kr = torch.empty_like(K) if Kr is None else Kr
+    _same_device(("Qr", Qr), ("Kr", Kr))
+    qs, ks = (B, H, N, d), (B, Hkv, N, d)
+    st = [_rows(Q, qs, Q.dtype, "Q"), _rows(K, ks, Q.dtype, "K"), _rows(Qr, qs, Q.dtype, "Qr"), _rows(Kr, ks, Q.dtype, "Kr")]
+    _check(lib.spark_qk_norm_rope_fwd(Q.data_ptr(), K.data_ptr(), *address, Qr.data_ptr(), Kr.data_ptr(), *st, *sizes,
+                                      _stream_ptr()))
+    return Qr, Kr
+
+
+def spark_qk_norm_rope_bwd_workspace_bytes(B: int, N: int, H: int, Hkv: int, d: int, rd: int, dtype_code: int) -> int:
+    return int(load_library().spark_qk_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, rd, dtype_code))
+
+
+def spark_qk_norm_rope_bwd(Q, K, wq, wk, cos, sin, dQr, dKr, positions=None, eps: float = 1e-6, interleaved: bool = False,
+                           dQ=None, dK=None, dwq=None, dwk=None, workspace=None):
+    """dQ, dK, dwq, dwk for the problem of spark_qk_norm_rope_fwd, whose Q and K must still hold the forward's inputs.
+    dwq and dwk are fp32."""
+    import torch
+    lib = load_library()
+    address, sizes = _qk_problem(Q, K, wq, wk, cos, sin, positions, eps, interleaved)
+    B, N, H, Hkv, d, rd = sizes[:6]
+    dQ = torch.empty_like(Q) if dQ is None else dQ
+    dK = torch.empty_like(K) if dK is None else dK
+    dwq = torch.empty(d, dtype=torch.float32, device=Q.device) if dwq is None else dwq
+    dwk = torch.empty(d, dtype=torch.float32, device=Q.device) if dwk is None else dwk
+    _same_device(("dQr", dQr), ("dKr", dKr), ("dQ", dQ), ("dK", dK), ("dwq", dwq), ("dwk", dwk), ("workspace", workspace))
+    for t, n in ((dwq, "dwq"), (dwk, "dwk")):
+        binding._require(t, (d,), torch.float32, n)
+    qs, ks = (B, H, N, d), (B, Hkv, N, d)
+    st = [_rows(Q, qs, Q.dtype, "Q"), _rows(K, ks, Q.dtype, "K"), _rows(dQr, qs, Q.dtype, "dQr"),
+          _rows(dKr, ks, Q.dtype, "dKr"), _rows(dQ, qs, Q.dtype, "dQ"), _rows(dK, ks, Q.dtype, "dK")]
+    need = spark_qk_norm_rope_bwd_workspace_bytes(B, N, H, Hkv, d, rd, sizes[-1])
+    workspace, nbytes = _scratch(workspace, need, Q)
+    _check(lib.spark_qk_norm_rope_bwd(Q.data_ptr(), K.data_ptr(), *address, dQr.data_ptr(), dKr.data_ptr(), dQ.data_ptr(),
+                                      dK.data_ptr(), dwq.data_ptr(), dwk.data_ptr(), *st, workspace.data_ptr(), nbytes,
+                                      *sizes, _stream_ptr()))
+    return dQ, dK, dwq, dwk
