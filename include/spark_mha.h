@@ -355,6 +355,37 @@ int spark_qk_norm_rope_bwd(const void* Q, const void* K, const void* wq, const v
                            float eps, int interleaved, int w_fp32, spark_dtype_t dtype, void* stream);
 
 /*
+ * Attention of a batch that shares long prefixes.  The B sequences come in G groups of B / G neighbours (sequence b is in
+ * group b / (B / G)).  A group's prefix exists once: Kp, Vp are [G,Hkv,P,d].  Behind it every sequence has a suffix of its
+ * own: Ks, Vs are [B,Hkv,S,d].  Q, O are [B,H,Nq,d], H a multiple of Hkv: query head h attends with head h / (H / Hkv) of
+ * the keys.  For query i of sequence b in group g, over the keys it sees,
+ *   O = softmax(scale * q . k) v,   LSE = ln sum exp(scale * q . k)   ([B,H,Nq] fp32),
+ * namely all prefix_lens[g] keys of the prefix, and of the suffix key j < s_lens[b], with causal != 0 only
+ * j <= i + s_lens[b] - q_lens[b] (the queries are the last tokens of the sequence).
+ *   prefix_lens [G], q_lens, s_lens [B] : in, device, int32; NULL: P, Nq, S.  Values are taken to be in 0 ... P (Nq, S);
+ *               others are cut to that.  Keys behind a length are never used, whatever stands there (NaN too).  Query rows
+ *               from q_lens[b] on are padding, and rows that see no key at all are allowed: both give O = 0, LSE = -inf.
+ * One new token per sequence is Nq = 1 with s_lens counting it; training on several answers to one prompt is Nq = S
+ * (q_lens = s_lens) with the prompt as prefix.
+ * Limits: P, S >= 0, not both 0 (a tensor of no rows may be NULL); Nq >= 1; B a multiple of G; d, scale, dtype and strides
+ * as in spark_mha_strided_fwd, except that the stride of an index with one value does not matter; B*H < 2^24 and
+ * B*H*ceil(max(Nq, P, S) / 32) < 2^31.  No dropout.
+ *   workspace : spark_mha_prefix_fwd_workspace_bytes(...) bytes of device memory, 16-byte aligned, contents unspecified on
+ *               return.  Few query rows per head of keys give too few workgroups unless several share the keys, and the rows
+ *               of a group's sequences are packed into common tiles: their partial results are kept there.  May be NULL (or
+ *               0 bytes be needed): same operation, every query tile by one workgroup.  SPARK_ERR_WORKSPACE if it is not
+ *               NULL and too small.
+ */
+size_t spark_mha_prefix_fwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, spark_dtype_t dtype);
+
+int spark_mha_prefix_fwd(const void* Q, const void* Kp, const void* Vp, const void* Ks, const void* Vs, void* O, float* LSE,
+                         const spark_strides_t* sQ, const spark_strides_t* sKp, const spark_strides_t* sVp,
+                         const spark_strides_t* sKs, const spark_strides_t* sVs, const spark_strides_t* sO,
+                         const int* prefix_lens, const int* q_lens, const int* s_lens, void* workspace,
+                         size_t workspace_bytes, int G, int B, int H, int Hkv, int Nq, int P, int S, int d, float scale,
+                         int causal, spark_dtype_t dtype, void* stream);
+
+/*
  * Hardware self-check of the register layouts the kernels are written against (wave64
  * 32x32x16 MFMA operands and accumulators, packed accumulator registers reused as the operand
  * of a second MFMA -- the register form of the paper's Sec. 3.2.2 layout transform -- and the

@@ -59,13 +59,37 @@ template <int D, int NW = 4, bool PAIR = false> struct FwdCfg {
   static_assert((STAGE & (STAGE - 1)) == 0, "XOR buffer switch");
 };
 
-// Workgroups per CU: at D = 64 three of four waves, which costs the causal kernel with dropout 8 of its 176 registers
-// (us, 256 heads x 2048 256 -> 236); at D = 128 the registers allow two.
-template <typename T, int D, bool CAUSAL, bool DROP, int NW = 4, bool PAIR = false>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_fwd_kernel(
+// The keys of a forward's query tile.  One sequence: rows 0 ... Nk-1 of K and V.
+struct OneSequence {
+  static constexpr bool PREFIX = false;
+  static constexpr int head = 0, item = 0, P = 0, rows = 0, ahead = 0;  // not used
+  static constexpr uint32_t kp_row_bytes = 0, vp_row_bytes = 0;
+  template <typename T>
+  __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap& m, int head, int H) const {
+    return X + head_base(m, head, H);
+  }
+};
+// Two: a prefix that other sequences share, and behind it the sequence's own suffix (K, V: of this head; Nk rows).  One of
+// them may be empty.  Tiles are walked in this order, so that those without a mask come first: the full tiles of the
+// prefix, the suffix, and the prefix's last tile if it is not full.  (Softmax does not mind the order of the keys.)
+template <typename T> struct PrefixAndSuffix {
+  static constexpr bool PREFIX = true;
+  int head, item;         // the workgroup's: b * H + h, query tile
+  const T *Kp, *Vp;       // of this head
+  uint32_t kp_row_bytes, vp_row_bytes;
+  uint32_t kp_bytes, vp_bytes;  // what the prefix spans
+  int P;                  // its keys
+  int rows;               // query rows in use, 1 at least; those behind, up to Nq, give zeros and an LSE of -inf
+  int ahead;              // query i sees suffix keys j <= i + ahead: causal, or a number that hides none
+  __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap&, int, int) const { return X; }
+};
+
+// The workgroup's part of the forward.
+template <typename T, int D, bool CAUSAL, bool DROP, int NW, bool PAIR, typename Keys>
+static __device__ __forceinline__ void fwd_tiles(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
     T* __restrict__ O, float* __restrict__ LSE, TensorMap mq, TensorMap mk, TensorMap mv,
-    TensorMap mo, int H, int Nq, int Nk, int dh, int nqt, int paired, float scale_log2, Dropout dr) {
+    TensorMap mo, int H, int Nq, int Nk, int dh, int nqt, int paired, float scale_log2, Dropout dr, Keys keys) {
   using F = Frag<T>;
   using v8 = typename F::v8;
   using v4 = typename F::v4;
@@ -95,16 +119,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
   // Work items.  Non-causal, or a causal grid too small for pairs: one query tile per workgroup.
   // Otherwise a causal workgroup takes the pair of tiles (nqt-1-p, p), whose loop lengths add up to
   // the same total for every p, so that all workgroups carry equal work and the launch has no
-  // tail of long tiles.
+  // tail of long tiles.  (With a prefix in front the lengths differ little, and the kernel maps its grid itself.)
   const int items = paired ? causal_items<CAUSAL>(nqt) : nqt;
   const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int head = logical / items;
-  const int item = logical - head * items;
+  const int head = Keys::PREFIX ? keys.head : logical / items;
+  const int item = Keys::PREFIX ? keys.item : logical - head * items;
 
   // Nq query rows and Nk key rows per head (equal for self-attention; causal needs them equal)
   const T* Qh = Q + head_base(mq, head, H);
-  const T* Kh = K + head_base(mk, head, H);
-  const T* Vh = V + head_base(mv, head, H);
+  const T* Kh = keys.head_rows(K, mk, head, H);
+  const T* Vh = keys.head_rows(V, mv, head, H);
+  // as k_lane_src, of the prefix
+  const uint32_t kp_lane_src = Keys::PREFIX ? dma_lane_src<D>(wave & 3, lane, keys.kp_row_bytes, dh) : 0;
+  const uint32_t vp_lane_src = Keys::PREFIX ? dma_lane_src<D>(wave & 3, lane, keys.vp_row_bytes, dh) : 0;
 
   for (int rep = 0; rep < (CAUSAL && paired ? 2 : 1); ++rep) {
     const int qt = CAUSAL && rep == 0 ? nqt - 1 - item : item;
@@ -115,27 +142,56 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
 
     const int q0 = qt * C::BM + wave * 32;  // first query row of this wave
     const int qrow = q0 + c32;              // this lane's query row
-    const int qrow_c = qrow < Nq ? qrow : Nq - 1;
+    const int q_end = Keys::PREFIX ? keys.rows : Nq;  // rows that attend
+    const int qrow_c = qrow < q_end ? qrow : q_end - 1;
 
     v8 qf[KS];
     load_row_frags(qf, Qh + (size_t)qrow_c * (size_t)mq.row, g, dh);
 
     int kv_end = Nk;
-    if (CAUSAL) {
+    if constexpr (Keys::PREFIX) {
+      const int lim = (qt + 1) * C::BM + keys.ahead;
+      kv_end = lim < 0 ? 0 : lim < Nk ? lim : Nk;
+    } else if (CAUSAL) {
       const int lim = (qt + 1) * C::BM;
       kv_end = lim < Nk ? lim : Nk;
     }
-    const int nt = (kv_end + C::BN - 1) / C::BN;
+    // with a prefix, tiles [0, np) are its full ones and [np_part, nt) its last one, if that is not full
+    const int np = Keys::PREFIX ? keys.P / C::BN : 0;
+    const int np_part = np + (kv_end + C::BN - 1) / C::BN;
+    const int nt = np_part + (Keys::PREFIX && keys.P % C::BN != 0);
 
     // K / V tiles: global -> LDS directly; rows past the end of the sequence arrive as zeros.  Tile t lives in slot
     // t mod SLOTS.
-    const BufView kview(Kh, head_span_bytes(mk, Nk, dh)), vview(Vh, head_span_bytes(mv, Nk, dh));
+    auto span = [&](const TensorMap& m, int n) { return Keys::PREFIX && n == 0 ? 0u : head_span_bytes(m, n, dh); };
+    const BufView kview(Kh, span(mk, Nk)), vview(Vh, span(mv, Nk));
+    // Tile t of a sequence in two parts: from the prefix if it is one of its tiles, else from the suffix.
+    auto fetch_part = [&](int t, const BufView& pre, const BufView& suf, int at, uint32_t pre_src, uint32_t suf_src,
+                          uint32_t pre_bytes, uint32_t suf_bytes) {
+      const bool of_prefix = t < np || t >= np_part;
+      const int r0 = (t < np ? t : t < np_part ? t - np : np) * C::BN;
+      SPARK_LDS char* const dst = smem + (t & (C::SLOTS - 1)) * C::STAGE + at;
+      if (of_prefix)
+        tile_dma<D, C::BN>(pre, r0, dst, wave, pre_src, pre_bytes);
+      else
+        tile_dma<D, C::BN>(suf, r0, dst, wave, suf_src, suf_bytes);
+    };
     auto fetch_k = [&](int t) {  // four waves move a tile
       if (t >= nt || (NW > 4 && wave >= 4)) return;
+      if constexpr (Keys::PREFIX) {
+        const BufView pview(keys.Kp, keys.kp_bytes);
+        fetch_part(t, pview, kview, 0, kp_lane_src, k_lane_src, keys.kp_row_bytes, k_row_bytes);
+        return;
+      }
       tile_dma<D, C::BN>(kview, t * C::BN, smem + (t & (C::SLOTS - 1)) * C::STAGE, wave, k_lane_src, k_row_bytes);
     };
     auto fetch_v = [&](int t) {
       if (t >= nt || (NW > 4 && wave >= 4)) return;
+      if constexpr (Keys::PREFIX) {
+        const BufView pview(keys.Vp, keys.vp_bytes);
+        fetch_part(t, pview, vview, C::TILE, vp_lane_src, v_lane_src, keys.vp_row_bytes, v_row_bytes);
+        return;
+      }
       tile_dma<D, C::BN>(vview, t * C::BN, smem + (t & (C::SLOTS - 1)) * C::STAGE + C::TILE, wave, v_lane_src,
                          v_row_bytes);
     };
@@ -167,7 +223,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
     // last key this lane's query attends to, less the 4 g that every register's key contains: the mask is one
     // compare with a constant per score (with both limits compared, four instructions; us, causal, d = 64, 256
     // heads x 512 22.8 -> 21.6, d = 80, 36 x 1333 35.9 -> 31.9)
-    const int last_key = (CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;
+    const int last_key = (Keys::PREFIX ? (qrow < Nk - keys.ahead ? qrow + keys.ahead : Nk - 1)
+                                       : (CAUSAL && qrow < Nk ? qrow : Nk - 1)) - 4 * g;
 
     // Carried from round to round: raw scores of the second half of tile i - 1, P of its first half and their sum.
     f32x16 s0, s1;
@@ -198,6 +255,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
         }
       };
 
+      // last_key as a position in the order in which the tiles are walked, for the half that starts at key0 there
+      auto last_at = [&](int key0) {
+        const int tile = key0 / C::BN;
+        if (tile >= np && tile < np_part) return last_key + np * C::BN;
+        return keys.P - 1 - 4 * g + (tile < np ? 0 : (np_part - np) * C::BN);
+      };
       float t[16];
       // Online softmax (Eq. 3) with a lazy reference point.  P is formed against the current
       // reference m_run straight away, WITHOUT computing the row maximum first; the row sum of the
@@ -209,6 +272,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
       // accumulators rescaled by exp(m_pre - m_cur) as in Eq. 3, and the half's P formed again.
       // key0: first key of the half.
       auto score = [&](const f32x16& s, int r, int key0) {
+        if constexpr (Keys::PREFIX) return MASKED && 8 * (r / 4) + (r % 4) > last_at(key0) - key0 ? -INFINITY : s[r];
         return MASKED && 8 * (r / 4) + (r % 4) > last_key - key0 ? -INFINITY : s[r];
       };
       auto exp_elem = [&](const f32x16& s, int r, int key0, float& rs) {
@@ -357,7 +421,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
     // row of this wave, and tiles from n_wave on are wholly above it.  Both differ between the waves of a workgroup; the
     // number of rounds, and with it the number of barriers, does not.
     int n_plain = Nk / C::BN, n_wave = nt;
-    if (CAUSAL) {
+    if constexpr (Keys::PREFIX) {
+      const int first = q0 + keys.ahead + 1;  // suffix keys that the wave's first row sees
+      if (first / C::BN < n_plain) n_plain = first < 0 ? 0 : first / C::BN;
+      if (n_plain > np_part - np) n_plain = np_part - np;
+      n_plain += np;
+      if (np_part == nt) {  // no tile of the prefix behind those of the suffix that the wave may leave out
+        const int seen = first + 30 < 0 ? 0 : (first + 30) / C::BN + 1;
+        if (np + seen < n_wave) n_wave = np + seen;
+        if (n_wave < 1) n_wave = 1;
+      }
+    } else if (CAUSAL) {
       if ((q0 + 1) / C::BN < n_plain) n_plain = (q0 + 1) / C::BN;
       if ((q0 + 31) / C::BN + 1 < n_wave) n_wave = (q0 + 31) / C::BN + 1;
     }
@@ -398,6 +472,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
     asm volatile("" : "+v"(elane));
     const int eg = elane >> 5, ec32 = column_row<LANES>(elane);
     l_run = half_pair_sum(l_run);
+    const bool empty = Keys::PREFIX && (l_run == 0.f || q0 + ec32 >= q_end);  // no key, or not a row in use: zeros
     const float inv = (DROP ? dr.rescale : 1.0f) / l_run;
     SPARK_LDS char* ob = smem + wave * 32 * C::OSTR;
 #pragma unroll
@@ -406,7 +481,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
       for (int r4 = 0; r4 < 4; ++r4) {
         v4 pk;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pk[e] = (T)(o[dt][r4 * 4 + e] * inv);
+        for (int e = 0; e < 4; ++e) pk[e] = (T)(empty ? 0.f : o[dt][r4 * 4 + e] * inv);
         lds_write(ob, ec32 * C::OSTR + (dt * 32 + 8 * r4 + 4 * eg) * 2, pk);
       }
     T* Oh = O + head_base(mo, head, H);
@@ -419,8 +494,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
         *reinterpret_cast<u32x4*>(Oh + (size_t)(q0 + row) * (size_t)mo.row + cc * 8) = v;
     }
     if (eg == 0 && q0 + ec32 < Nq)
-      LSE[(size_t)head * Nq + q0 + ec32] = (m_run + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f;
+      LSE[(size_t)head * Nq + q0 + ec32] = empty ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.6931471805599453f;
   }  // rep
+}
+
+// Workgroups per CU: at D = 64 three of four waves, which costs the causal kernel with dropout 8 of its 176 registers
+// (us, 256 heads x 2048 256 -> 236); at D = 128 the registers allow two.
+template <typename T, int D, bool CAUSAL, bool DROP, int NW = 4, bool PAIR = false>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_fwd_kernel(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
+    T* __restrict__ O, float* __restrict__ LSE, TensorMap mq, TensorMap mk, TensorMap mv,
+    TensorMap mo, int H, int Nq, int Nk, int dh, int nqt, int paired, float scale_log2, Dropout dr) {
+  fwd_tiles<T, D, CAUSAL, DROP, NW, PAIR>(Q, K, V, O, LSE, mq, mk, mv, mo, H, Nq, Nk, dh, nqt, paired, scale_log2, dr,
+                                          OneSequence{});
 }
 
 }  // namespace spark

@@ -126,3 +126,49 @@ def spark_qk_norm_rope_bwd(Q, K, wq, wk, cos, sin, dQr, dKr, positions=None, eps
                                       dK.data_ptr(), dwq.data_ptr(), dwk.data_ptr(), *st, workspace.data_ptr(), nbytes,
                                       *sizes, _stream_ptr()))
     return dQ, dK, dwq, dwk
+
+
+def _prefix_problem(Q, Kp, Vp, Ks, Vs, prefix_lens, q_lens, s_lens):
+    """(sizes G, B, H, Hkv, Nq, P, S, d; strides of the five tensors; addresses of the lengths)"""
+    for t, n in ((Q, "Q"), (Kp, "Kp"), (Vp, "Vp"), (Ks, "Ks"), (Vs, "Vs")):
+        if t.dim() != 4:
+            raise ValueError("%s must have four dimensions" % n)
+    _same_device(("Q", Q), ("Kp", Kp), ("Vp", Vp), ("Ks", Ks), ("Vs", Vs), ("prefix_lens", prefix_lens), ("q_lens", q_lens),
+                 ("s_lens", s_lens))
+    B, H, Nq, d = Q.shape
+    G, Hkv, P = Kp.shape[:3]
+    S = Ks.shape[2]
+    _dtype_code(Q)
+    strides = [_rows(Q, (B, H, Nq, d), Q.dtype, "Q")]
+    strides += [_rows(t, (G, Hkv, P, d), Q.dtype, n) for t, n in ((Kp, "Kp"), (Vp, "Vp"))]
+    strides += [_rows(t, (B, Hkv, S, d), Q.dtype, n) for t, n in ((Ks, "Ks"), (Vs, "Vs"))]
+    lens = [_ints(prefix_lens, (G,), "prefix_lens"), _ints(q_lens, (B,), "q_lens"), _ints(s_lens, (B,), "s_lens")]
+    return (G, B, H, Hkv, Nq, P, S, d), strides, lens
+
+
+def spark_mha_prefix_fwd_workspace_bytes(G: int, B: int, H: int, Hkv: int, Nq: int, P: int, S: int, d: int,
+                                         dtype_code: int) -> int:
+    return int(load_library().spark_mha_prefix_fwd_workspace_bytes(G, B, H, Hkv, Nq, P, S, d, dtype_code))
+
+
+def spark_mha_prefix_fwd(Q, Kp, Vp, Ks, Vs, scale: float, causal: bool = True, prefix_lens=None, q_lens=None, s_lens=None,
+                         O=None, LSE=None, workspace=None):
+    """O, LSE of Q [B,H,Nq,d] attending to the prefix Kp, Vp [G,Hkv,P,d] that B / G sequences in a row share, and to their
+    own suffixes Ks, Vs [B,Hkv,S,d].  prefix_lens [G], q_lens, s_lens [B]: int32 on the device, how much of P, Nq, S is in
+    use.  causal: query i sees suffix keys j <= i + s_lens - q_lens.  Rows from q_lens on, and rows that see no key, give
+    O = 0 and LSE = -inf.  Any strides."""
+    import torch
+    lib = load_library()
+    sizes, strides, lens = _prefix_problem(Q, Kp, Vp, Ks, Vs, prefix_lens, q_lens, s_lens)
+    G, B, H, Hkv, Nq, P, S, d = sizes
+    code = _dtype_code(Q)
+    O = torch.empty_like(Q) if O is None else O
+    LSE = torch.empty((B, H, Nq), dtype=torch.float32, device=Q.device) if LSE is None else LSE
+    _same_device(("O", O), ("LSE", LSE), ("workspace", workspace))
+    strides.append(_rows(O, (B, H, Nq, d), Q.dtype, "O"))
+    binding._require(LSE, (B, H, Nq), torch.float32, "LSE")
+    workspace, nbytes = _scratch(workspace, spark_mha_prefix_fwd_workspace_bytes(*sizes, code), Q)
+    _check(lib.spark_mha_prefix_fwd(Q.data_ptr(), Kp.data_ptr(), Vp.data_ptr(), Ks.data_ptr(), Vs.data_ptr(), O.data_ptr(),
+                                    LSE.data_ptr(), *strides, *lens, workspace.data_ptr(), nbytes, *sizes, float(scale),
+                                    int(bool(causal)), code, _stream_ptr()))
+    return O, LSE
