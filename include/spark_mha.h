@@ -386,6 +386,28 @@ int spark_mha_prefix_fwd(const void* Q, const void* Kp, const void* Vp, const vo
                          int causal, spark_dtype_t dtype, void* stream);
 
 /*
+ * Its backward, from the O and LSE that the forward wrote (with the same lengths).  All gradients are fully overwritten:
+ * rows of dQ from q_lens on, and rows of dKp, dVp (dKs, dVs) behind prefix_lens (s_lens) or seen by no query, with zeros.
+ * dKp and dVp sum over all sequences of the group, dKs and dVs over the query heads that share a head of keys.  The order of
+ * the sums depends on the sizes alone: results are the same bit for bit in every run.  dO of rows in use must be finite.
+ *   O, dO, dQ : [B,H,Nq,d];   dKp, dVp : [G,Hkv,P,d];   dKs, dVs : [B,Hkv,S,d]
+ *   workspace : device scratch of at least spark_mha_prefix_bwd_workspace_bytes(...) bytes, 16-byte aligned (D and
+ *               LSE * log2(e) of every row, and the parts of dKp, dVp where several workgroups share a tile's rows)
+ */
+size_t spark_mha_prefix_bwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, int causal,
+                                            spark_dtype_t dtype);
+
+int spark_mha_prefix_bwd(const void* Q, const void* Kp, const void* Vp, const void* Ks, const void* Vs, const void* O,
+                         const float* LSE, const void* dO, void* dQ, void* dKp, void* dVp, void* dKs, void* dVs,
+                         const spark_strides_t* sQ, const spark_strides_t* sKp, const spark_strides_t* sVp,
+                         const spark_strides_t* sKs, const spark_strides_t* sVs, const spark_strides_t* sO,
+                         const spark_strides_t* sdO, const spark_strides_t* sdQ, const spark_strides_t* sdKp,
+                         const spark_strides_t* sdVp, const spark_strides_t* sdKs, const spark_strides_t* sdVs,
+                         const int* prefix_lens, const int* q_lens, const int* s_lens, void* workspace,
+                         size_t workspace_bytes, int G, int B, int H, int Hkv, int Nq, int P, int S, int d, float scale,
+                         int causal, spark_dtype_t dtype, void* stream);
+
+/*
  * Hardware self-check of the register layouts the kernels are written against (wave64
  * 32x32x16 MFMA operands and accumulators, packed accumulator registers reused as the operand
  * of a second MFMA -- the register form of the paper's Sec. 3.2.2 layout transform -- and the

@@ -30,6 +30,8 @@ from .binding import (  # noqa: F401
     status_str,
 )
 from .decoder import (  # noqa: F401
+    spark_mha_prefix_bwd,
+    spark_mha_prefix_bwd_workspace_bytes,
     spark_mha_prefix_fwd,
     spark_mha_prefix_fwd_workspace_bytes,
     spark_qk_norm_rope_bwd,

@@ -29,7 +29,8 @@ EXPORTS = ("spark_mha_fwd", "spark_mha_bwd", "spark_mha_bwd_marked",
            "spark_mha_bwd_atomic_workspace_bytes", "spark_mha_dropout_bwd_marked",
            "spark_mha_workspace_fwd", "spark_mha_fwd_workspace_bytes", "spark_mha_bwd_grids",
            "spark_qk_norm_rope_fwd", "spark_qk_norm_rope_bwd", "spark_qk_norm_rope_bwd_workspace_bytes",
-           "spark_mha_prefix_fwd", "spark_mha_prefix_fwd_workspace_bytes")
+           "spark_mha_prefix_fwd", "spark_mha_prefix_fwd_workspace_bytes",
+           "spark_mha_prefix_bwd", "spark_mha_prefix_bwd_workspace_bytes")
 
 _lib = None
 _host = None  # the extension module; loaded together with the library
@@ -148,6 +149,10 @@ def load_library() -> ctypes.CDLL:
     lib.spark_mha_prefix_fwd_workspace_bytes.argtypes = [i] * 9
     lib.spark_mha_prefix_fwd.restype = i
     lib.spark_mha_prefix_fwd.argtypes = [vp] * 7 + [sp] * 6 + [vp] * 4 + [ctypes.c_size_t] + [i] * 8 + [f, i, i, vp]
+    lib.spark_mha_prefix_bwd_workspace_bytes.restype = ctypes.c_size_t
+    lib.spark_mha_prefix_bwd_workspace_bytes.argtypes = [i] * 10
+    lib.spark_mha_prefix_bwd.restype = i
+    lib.spark_mha_prefix_bwd.argtypes = [vp] * 13 + [sp] * 12 + [vp] * 4 + [ctypes.c_size_t] + [i] * 8 + [f, i, i, vp]
     lib.spark_layout_probe.restype = i
     lib.spark_layout_probe.argtypes = [vp, i, vp]
     lib.spark_status_str.restype = ctypes.c_char_p

@@ -29,6 +29,7 @@
 // scalars and dS^T is directly the B operand of dQ^T = K^T dS^T.
 #pragma once
 #include "dropout_gfx950.hpp"
+#include "fwd_kernel.hpp"
 #include "mma_gfx950.hpp"
 #include "tiles_gfx950.hpp"
 
@@ -74,14 +75,19 @@ static __device__ __forceinline__ float dropout_ds(uint32_t keep, float pe, floa
   return pe * (keep_float(keep, dp) + d);
 }
 
+// The query rows that the dK/dV loop walks.  One head's: rows 0 ... Nq-1.  (Several heads' and sequences': prefix_kernels.hpp.)
+struct OneHead {
+  static constexpr bool SEVERAL = false;
+};
+
 // The workgroup's part: key tile `item` of `head`, and its partner if the causal tiles are paired.
-template <typename T, int D, bool CAUSAL, bool DROP, Lanes M, bool COMPARE = false>
+template <typename T, int D, bool CAUSAL, bool DROP, Lanes M, bool COMPARE = false, typename Rows = OneHead>
 static __device__ __forceinline__ void bwd_dkdv_pipe(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
     const T* __restrict__ dO, const float* __restrict__ LSE2, const float* __restrict__ Dws,
     T* __restrict__ dK, T* __restrict__ dV, const TensorMap& mq, const TensorMap& mk, const TensorMap& mv,
     const TensorMap& mdo, const TensorMap& mdk, const TensorMap& mdv, int H, int Nq, int Nk, int dh, int nkt,
-    int paired, float scale, const Dropout& dr, int head, int item) {
+    int paired, float scale, const Dropout& dr, int head, int item, Rows rows = Rows{}) {
   using F = Frag<T>;
   using v8 = typename F::v8;
   using C = BwdKvPipeCfg<D>;
@@ -97,6 +103,7 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
 
   const T* Kh = K + head_base(mk, head, H);
   const T* Vh = V + head_base(mv, head, H);
+  // (for several heads' rows K, V are the head's own, and Q, dO come from `rows`)
   const BufView qview(Q + head_base(mq, head, H), head_span_bytes(mq, Nq, dh));
   const BufView doview(dO + head_base(mdo, head, H), head_span_bytes(mdo, Nq, dh));
   const uint32_t q_row_bytes = (uint32_t)mq.row * 2, do_row_bytes = (uint32_t)mdo.row * 2;
@@ -132,8 +139,10 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
 #pragma unroll
       for (int r = 0; r < 16; ++r) { dk[dt][r] = 0.f; dv[dt][r] = 0.f; }
 
+    // Several heads' rows: `rows` hands out their stages one after the other, and the loop ends with the last one (ns is
+    // not used); stage numbers only count.
     const int ns = (Nq + C::BM - 1) / C::BM;
-    const int s_begin = CAUSAL ? (kt * C::BN) / C::BM : 0;
+    const int s_begin = CAUSAL && !Rows::SEVERAL ? (kt * C::BN) / C::BM : 0;
 
     const LaneOffsets lane_off(lane);  // offsets inside slot 0
     const int lane_stat = C::STAT0 + 16 * g;
@@ -141,6 +150,16 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
     // global -> LDS slot, asynchronously (completion is awaited with wait_vmem_all + barrier)
     auto fetch_stage = [&](int m, int slot) {
       SPARK_LDS char* sb = smem + slot * C::STAGE;
+      if constexpr (Rows::SEVERAL) {
+        const auto s = rows.stage();
+        const int r0 = s.block * C::BM;
+        tile_dma<D, C::BM>(BufView(s.q, s.q_bytes), r0, sb, wave, q_lane_src, q_row_bytes);
+        tile_dma<D, C::BM>(BufView(s.dout, s.do_bytes), r0, sb + C::TILE, wave, do_lane_src, do_row_bytes);
+        SPARK_LDS char* st = smem + C::STAT0 + slot * C::STAT;
+        if (wave == 0) BufView(s.lse2, s.stat_bytes).load4_to_lds(st, lane * 4, (uint32_t)r0 * 4);
+        if (wave == 1) BufView(s.dws, s.stat_bytes).load4_to_lds(st + C::BM * 4, lane * 4, (uint32_t)r0 * 4);
+        return;
+      }
       tile_dma<D, C::BM>(qview, m * C::BM, sb, wave, q_lane_src, q_row_bytes);
       tile_dma<D, C::BM>(doview, m * C::BM, sb + C::TILE, wave, do_lane_src, do_row_bytes);
       // 64 floats of LSE*log2(e) (wave 0) and of D (wave 1): 4 bytes per lane
@@ -268,8 +287,18 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
     uint32_t kbCur[4] = {0, 0, 0, 0}, kbNew[4] = {0, 0, 0, 0};  // decision bytes of the current / next step
 
     // ---- prologue: stages s_begin and s_begin+1 resident, scores of the first step formed ----
+    // first query of the present stage and the next as the causal mask counts them (several heads' rows only)
+    int at = 0, at_next = 0;
+    bool more = true, has_next = false;
+    if constexpr (Rows::SEVERAL) at = rows.first_query();
     fetch_stage(s_begin, 0);
-    if (s_begin + 1 < ns) fetch_stage(s_begin + 1, 1);
+    if constexpr (Rows::SEVERAL) {
+      has_next = rows.advance();
+      at_next = rows.first_query();
+      if (has_next) fetch_stage(s_begin + 1, 1);
+    } else if (s_begin + 1 < ns) {
+      fetch_stage(s_begin + 1, 1);
+    }
     wait_vmem_all();
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(kf[ks]), "+v"(vf[ks]));
@@ -312,7 +341,7 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
     {
       float p[8], ds[8];
       uint32_t pk_p[4], pk_ds[4];
-      const int ahead_first = CAUSAL ? ahead_of(s_begin * C::BM) : 0;
+      const int ahead_first = CAUSAL ? ahead_of(Rows::SEVERAL ? at : s_begin * C::BM) : 0;
       if (DROP) keep_bytes_key_lane<M>(dr, head, krow, s_begin * C::BM, lane, kbCur);
 #pragma unroll
       for (int r = 0; r < 8; ++r)
@@ -334,7 +363,16 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
       const int slot1 = slot == 2 ? 0 : slot + 1;
       const int slot2 = slot1 == 2 ? 0 : slot1 + 1;
       // stage m+2 goes into the slot that stage m-1 used; everybody left it before the last barrier
-      if (m + 2 < ns) fetch_stage(m + 2, slot2);
+      int q0 = m * C::BM, q0_next = q0 + C::BM;
+      bool has_second = false;
+      if constexpr (Rows::SEVERAL) {
+        q0 = at;
+        q0_next = at_next;
+        has_second = has_next && rows.advance();
+        if (has_second) fetch_stage(m + 2, slot2);
+      } else if (m + 2 < ns) {
+        fetch_stage(m + 2, slot2);
+      }
 
       // One step.  cur: scores complete, first half of P / dS packed.  new: the step after it
       // (sub_new inside the stage offA / statA point at).
@@ -426,21 +464,41 @@ static __device__ __forceinline__ void bwd_dkdv_pipe(
       };
       auto request_A = [&](int part) { load_agroup(part, 1); };
       sched_fence();
-      step(sY, dpY, 1, m * C::BM + 32, sX, dpX, 0, m * C::BM, request_B);
+      step(sY, dpY, 1, q0 + 32, sX, dpX, 0, q0, request_B);
       // (m+1, 0) scores  ||  (m, 1) softmax; then (m, 1) dV / dK
 #pragma unroll
       for (int r = 0; r < 16; ++r) sX[r] = 0.f;
       dpX = dp_start(0);  // statA points at stage m + 1 by now (request_B moved it)
       sched_fence();
-      step(sX, dpX, 0, (m + 1) * C::BM, sY, dpY, 1, m * C::BM + 32, request_A);
+      step(sX, dpX, 0, q0_next, sY, dpY, 1, q0 + 32, request_A);
 
       point_C(slot1);
+      if constexpr (Rows::SEVERAL) {
+        at = at_next;
+        at_next = rows.first_query();
+        more = has_next;
+        has_next = has_second;
+      }
       wait_vmem_all();  // stage m+2 has landed (it was requested a whole stage ago)
       __syncthreads();
     };
 
     int m = s_begin, slot = 0;
-    if (CAUSAL) {  // the diagonal crosses the first two stages only
+    if constexpr (Rows::SEVERAL) {
+      // a stage's mask covers it and the first step of the next; key k0w + 127 is the last of any wave's
+      const int last = kt * C::BN + C::BN - 1;
+      while (more) {
+        if constexpr (CAUSAL) {
+          stage(m, slot, at < last || (has_next && at_next < last));
+        } else {
+          stage(m, slot, false);
+        }
+        ++m;
+        slot = slot == 2 ? 0 : slot + 1;
+      }
+      rows.store(dk, dv, smem + wave * 32 * C::OSTR, k0w, lane, scale);
+      return;
+    } else if (CAUSAL) {  // the diagonal crosses the first two stages only
       const int m_end = s_begin + 2 < ns ? s_begin + 2 : ns;
       for (; m < m_end; ++m) {
         stage(m, slot, true);
@@ -512,14 +570,14 @@ template <int D, bool CAUSAL, bool DROP> struct BwdQCfg {
 // The workgroup's part: query tile `item` of `head`, and its partner if the causal tiles are paired.
 // STATS: the workspace holds -D and LSE * log2(e) already (mha_bwd_stats_kernel); otherwise they are
 // formed here and left there for the dK/dV kernel.
-template <typename T, int D, bool CAUSAL, bool DROP, bool STATS, Lanes M>
+template <typename T, int D, bool CAUSAL, bool DROP, bool STATS, Lanes M, typename Keys = OneSequence>
 static __device__ __forceinline__ void bwd_dq(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
     const T* __restrict__ O, const T* __restrict__ dO, const float* __restrict__ LSE,
     float* __restrict__ Dws, float* __restrict__ LSE2ws, T* __restrict__ dQ, const TensorMap& mq,
     const TensorMap& mk, const TensorMap& mv, const TensorMap& mo, const TensorMap& mdo, const TensorMap& mdq, int H,
     int Nq, int Nk, int dh, int nqt, int paired, float scale, float scale_log2, const Dropout& dr, int head,
-    int item) {
+    int item, Keys keys = Keys{}) {
   using F = Frag<T>;
   using v8 = typename F::v8;
   using C = BwdQCfg<D, CAUSAL, DROP>;
@@ -539,14 +597,28 @@ static __device__ __forceinline__ void bwd_dq(
   const T* Qh = Q + head_base(mq, head, H);
   const T* dOh = dO + head_base(mdo, head, H);
   const T* Oh = STATS ? nullptr : O + head_base(mo, head, H);
-  const BufView kview(K + head_base(mk, head, H), head_span_bytes(mk, Nk, dh));
-  const BufView vview(V + head_base(mv, head, H), head_span_bytes(mv, Nk, dh));
+  const BufView kview(keys.head_rows(K, mk, head, H), Keys::PREFIX && Nk == 0 ? 0u : head_span_bytes(mk, Nk, dh));
+  const BufView vview(keys.head_rows(V, mv, head, H), Keys::PREFIX && Nk == 0 ? 0u : head_span_bytes(mv, Nk, dh));
   const uint32_t k_row_bytes = (uint32_t)mk.row * 2, v_row_bytes = (uint32_t)mv.row * 2;
   const uint32_t k_lane_src = dma_lane_src<D>(wave, lane, k_row_bytes, dh);
   const uint32_t v_lane_src = dma_lane_src<D>(wave, lane, v_row_bytes, dh);
   // K / V tiles go global -> LDS directly (no staging registers, no LDS store instructions);
   // completion is awaited with wait_vmem_all + barrier at the end of the iteration before use.
+  // With a prefix, tiles [0, np) are its full ones and those from np_part on its last one, if that is not full.
+  const int np = Keys::PREFIX ? keys.P / C::BN : 0;
+  int np_part = 0;
   auto fetch_tile = [&](int j, int buf) {
+    if constexpr (Keys::PREFIX) {
+      if (j < np || j >= np_part) {
+        const int r0 = (j < np ? j : np) * C::BN;
+        tile_dma<D, C::BN>(BufView(keys.Kp, keys.kp_bytes), r0, smem + buf * C::STAGE, wave,
+                           dma_lane_src<D>(wave, lane, keys.kp_row_bytes, dh), keys.kp_row_bytes);
+        tile_dma<D, C::BN>(BufView(keys.Vp, keys.vp_bytes), r0, smem + buf * C::STAGE + C::TILE, wave,
+                           dma_lane_src<D>(wave, lane, keys.vp_row_bytes, dh), keys.vp_row_bytes);
+        return;
+      }
+      j -= np;
+    }
     tile_dma<D, C::BN>(kview, j * C::BN, smem + buf * C::STAGE, wave, k_lane_src, k_row_bytes);
     tile_dma<D, C::BN>(vview, j * C::BN, smem + buf * C::STAGE + C::TILE, wave, v_lane_src, v_row_bytes);
   };
@@ -559,7 +631,8 @@ static __device__ __forceinline__ void bwd_dq(
     }
     const int q0 = qt * C::BM + wave * 32;
     const int qrow = q0 + c32;
-    const int qrow_c = qrow < Nq ? qrow : Nq - 1;
+    const int q_end = Keys::PREFIX ? keys.rows : Nq;  // rows that attend
+    const int qrow_c = qrow < q_end ? qrow : q_end - 1;
 
     v8 qf[KS], dof[KS], of[KS];  // of: the row of O, needed for D only
     if constexpr (CAUSAL) {
@@ -576,11 +649,15 @@ static __device__ __forceinline__ void bwd_dq(
     float Dq = STATS ? -Dws[(size_t)head * Nq + qrow_c] : 0.f;
 
     int kv_end = Nk;
-    if (CAUSAL) {
+    if constexpr (Keys::PREFIX) {
+      const int lim = (qt + 1) * C::BM + keys.ahead;
+      kv_end = lim < 0 ? 0 : lim < Nk ? lim : Nk;
+    } else if (CAUSAL) {
       const int lim = (qt + 1) * C::BM;
       kv_end = lim < Nk ? lim : Nk;
     }
-    const int nt = (kv_end + C::BN - 1) / C::BN;
+    if constexpr (Keys::PREFIX) np_part = np + (kv_end + C::BN - 1) / C::BN;
+    const int nt = Keys::PREFIX ? np_part + (keys.P % C::BN != 0) : (kv_end + C::BN - 1) / C::BN;
 
     LaneOffsets off(lane);  // read offsets of the current buffer
 
@@ -606,7 +683,8 @@ static __device__ __forceinline__ void bwd_dq(
         for (int i = 0; i < 8; ++i) Dq = __builtin_fmaf((float)of[ks][i], (float)dof[ks][i], Dq);
       Dq = half_pair_sum(Dq) * (DROP ? dr.keep_prob : 1.0f);
       lse2 *= 1.4426950408889634f;
-      if (g == 0 && qrow < Nq) {
+      if (Keys::PREFIX && lse2 == -INFINITY) lse2 = INFINITY;  // a row without keys: P = exp2(s - inf) = 0
+      if (g == 0 && qrow < q_end) {
         Dws[(size_t)head * Nq + qrow] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
         LSE2ws[(size_t)head * Nq + qrow] = lse2;
       }
@@ -626,16 +704,19 @@ static __device__ __forceinline__ void bwd_dq(
 
     // last key this lane's query attends to, less the 4 g that every register's key contains: the mask is one
     // compare with a constant per element
-    const int last_key = (CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;
+    const int last_key = (Keys::PREFIX ? (qrow < Nk - keys.ahead ? qrow + keys.ahead : Nk - 1)
+                                       : (CAUSAL && qrow < Nk ? qrow : Nk - 1)) - 4 * g;
     // One iteration, compiled twice: MASKED for tiles that the diagonal or the end of the keys
     // crosses, and without any mask arithmetic for all the others.
     auto iteration = [&](const int j, auto masked_tag) {
       constexpr bool MASKED = decltype(masked_tag)::value;
       const int buf = j & 1;
       if (j + 1 < nt) fetch_tile(j + 1, buf ^ 1);  // everybody left that buffer before the last barrier
-      const int k0 = j * C::BN;
+      // with a prefix: first key of the tile in its part, and whether the part is the prefix
+      const bool of_prefix = Keys::PREFIX && (j < np || j >= np_part);
+      const int k0 = (!Keys::PREFIX ? j : of_prefix ? (j < np ? j : np) : j - np) * C::BN;
       // wave-uniform: skip tiles entirely above the diagonal (they are among the masked ones)
-      if (!MASKED || !CAUSAL || k0 <= q0 + 31) {
+      if (!MASKED || !CAUSAL || of_prefix || k0 <= q0 + 31 + keys.ahead) {
         SPARK_LDS const char* kb = smem;  // + off.* (which carry the buffer bit)
         SPARK_LDS const char* vb = smem + C::TILE;
 
@@ -695,7 +776,8 @@ static __device__ __forceinline__ void bwd_dq(
         auto p_elem = [&](int e) {  // e = mt * 16 + r
           const int mt = e / 16, r = e % 16;
           float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][r], scale_log2, -lse2));
-          if (MASKED) x = mt * 32 + 8 * (r / 4) + (r % 4) > last_key - k0 ? 0.f : x;
+          if (MASKED)
+            x = mt * 32 + 8 * (r / 4) + (r % 4) > (of_prefix ? keys.P - 1 - 4 * g : last_key) - k0 ? 0.f : x;
           pe[e] = x;
           asm volatile("" : "+v"(pe[e]));
         };
@@ -775,11 +857,24 @@ static __device__ __forceinline__ void bwd_dq(
     // row of this wave.  The split differs between the waves of a workgroup; the number of
     // iterations, and with it the number of barriers, does not.
     int n_plain = Nk / C::BN;
-    if (CAUSAL && (q0 + 1) / C::BN < n_plain) n_plain = (q0 + 1) / C::BN;
+    if constexpr (Keys::PREFIX) {
+      const int first = q0 + keys.ahead + 1;  // suffix keys that the wave's first row sees
+      if (first / C::BN < n_plain) n_plain = first < 0 ? 0 : first / C::BN;
+      n_plain += np;
+      if (n_plain > np_part) n_plain = np_part;
+    } else if (CAUSAL && (q0 + 1) / C::BN < n_plain) {
+      n_plain = (q0 + 1) / C::BN;
+    }
     if (n_plain > nt) n_plain = nt;
     int j = 0;
     for (; j < n_plain; ++j) iteration(j, std::false_type{});
     for (; j < nt; ++j) iteration(j, std::true_type{});
+    if constexpr (Keys::PREFIX) {  // rows not in use: zeros
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dq[dt][r] = qrow < q_end ? dq[dt][r] : 0.f;
+    }
 
     SPARK_LDS char* ob = smem + wave * 32 * C::OSTR;
     store_transposed<T, D, C::OSTR, M>(dq, DROP ? scale * dr.rescale : scale, ob, dQ + head_base(mdq, head, H), q0,

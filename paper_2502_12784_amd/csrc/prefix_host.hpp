@@ -52,9 +52,130 @@ int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, float scale
   return launch_prefix_fwd<T, 128, 4, false>(p, O, LSE, scale, st);
 }
 
+// Workgroups that share the rows of a prefix tile: enough that such a tile takes no longer than its share of the chip's
+// work, all of a workgroup's stages counted alike (a suffix tile's rows, if causal, as half).
+int prefix_parts(const PrefixProblem& p) {
+  if (p.P == 0) return 1;
+  const int64_t slots = 256 * (p.dh <= 64 ? 2 : 1), pairs = (int64_t)(p.B / p.G) * (p.H / p.Hkv), blocks = (p.Nq + 63) / 64;
+  const int64_t n1 = (int64_t)p.G * p.Hkv * ((p.P + 127) / 128), n2 = (int64_t)p.B * p.Hkv * ((p.S + 127) / 128);
+  const int64_t w1 = pairs * blocks, w2 = (p.H / p.Hkv) * blocks;
+  const int64_t share = (n1 * w1 + n2 * w2 / (p.causal ? 2 : 1)) / slots + 1;
+  int64_t parts = (w1 + share - 1) / share;
+  if (parts > 32) parts = 32;
+  if (parts > pairs) parts = pairs;
+  if (n1 * parts >= (int64_t)1 << 30) parts = 1;
+  return parts < 1 ? 1 : (int)parts;
+}
+size_t prefix_stats_bytes(const PrefixProblem& p) { return ((size_t)p.B * p.H * p.Nq * 8 + 255) & ~(size_t)255; }
+size_t prefix_bwd_workspace(const PrefixProblem& p) {
+  const int parts = prefix_parts(p);
+  const size_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
+  return prefix_stats_bytes(p) + (parts > 1 ? (size_t)parts * p.G * p.Hkv * p.P * columns * 8 : 0);
+}
+
+template <typename T, int D>
+int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, float scale, hipStream_t st) {
+  {
+    using C = BwdQCfg<D, true, false>;
+    auto kernel = mha_prefix_dq_kernel<T, D>;
+    static std::atomic<uint64_t> ready{0};
+    const int attr = ensure_smem(kernel, C::SMEM, ready);
+    if (attr != SPARK_OK) return attr;
+    const int nqt = (p.Nq + C::BM - 1) / C::BM;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.H * nqt)), dim3(256), C::SMEM, st, p, static_cast<const T*>(O), gr, nqt,
+                       scale);
+    if (!launch_ok("dQ kernel (prefix)")) return SPARK_ERR_LAUNCH;
+  }
+  using C = BwdKvPipeCfg<D>;
+  auto kernel = mha_prefix_dkdv_kernel<T, D>;
+  static std::atomic<uint64_t> ready{0};
+  const int attr = ensure_smem(kernel, C::SMEM, ready);
+  if (attr != SPARK_OK) return attr;
+  const int p_tiles = (p.P + C::BN - 1) / C::BN, s_tiles = (p.S + C::BN - 1) / C::BN;
+  const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), C::SMEM, st, p, gr, p_tiles, s_tiles, first, scale);
+  if (!launch_ok("dK/dV kernel (prefix)")) return SPARK_ERR_LAUNCH;
+  if (gr.parts == 1) return SPARK_OK;
+  constexpr int RPB = 256 * 4 / D;
+  const int64_t rows = (int64_t)p.G * p.Hkv * p.P;
+  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, st, p, gr, scale);
+  return launch_ok("sum of the prefix's parts") ? SPARK_OK : SPARK_ERR_LAUNCH;
+}
+
+struct PrefixGradArgs {
+  const void* dO;
+  void *dQ, *dKp, *dVp, *dKs, *dVs;
+  TensorMap mdo, mdq, mdkp, mdvp, mdks, mdvs;
+  const float* LSE;
+  void* workspace;
+};
+
+template <typename T>
+int dispatch_prefix_bwd(const PrefixProblem& p, const void* O, const PrefixGradArgs& a, float scale, hipStream_t st) {
+  PrefixGrads<T> gr;
+  gr.dO = static_cast<const T*>(a.dO);
+  gr.dQ = static_cast<T*>(a.dQ);
+  gr.dKp = static_cast<T*>(a.dKp);
+  gr.dVp = static_cast<T*>(a.dVp);
+  gr.dKs = static_cast<T*>(a.dKs);
+  gr.dVs = static_cast<T*>(a.dVs);
+  gr.mdo = a.mdo; gr.mdq = a.mdq; gr.mdkp = a.mdkp; gr.mdvp = a.mdvp; gr.mdks = a.mdks; gr.mdvs = a.mdvs;
+  gr.LSE = a.LSE;
+  gr.Dws = static_cast<float*>(a.workspace);
+  gr.LSE2ws = gr.Dws + (size_t)p.B * p.H * p.Nq;
+  gr.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + prefix_stats_bytes(p));
+  gr.parts = prefix_parts(p);
+  if (p.dh <= 64) return launch_prefix_bwd<T, 64>(p, O, gr, scale, st);
+  if (p.dh <= 96) return launch_prefix_bwd<T, 96>(p, O, gr, scale, st);
+  return launch_prefix_bwd<T, 128>(p, O, gr, scale, st);
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t spark_mha_prefix_bwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, int causal,
+                                            spark_dtype_t dtype) {
+  PrefixProblem p{};
+  if (make_prefix(&p, G, B, H, Hkv, Nq, P, S, d, 1.0f, causal, (int)dtype) != SPARK_OK) return 0;
+  return prefix_bwd_workspace(p);
+}
+
+int spark_mha_prefix_bwd(const void* Q, const void* Kp, const void* Vp, const void* Ks, const void* Vs, const void* O,
+                         const float* LSE, const void* dO, void* dQ, void* dKp, void* dVp, void* dKs, void* dVs,
+                         const spark_strides_t* sQ, const spark_strides_t* sKp, const spark_strides_t* sVp,
+                         const spark_strides_t* sKs, const spark_strides_t* sVs, const spark_strides_t* sO,
+                         const spark_strides_t* sdO, const spark_strides_t* sdQ, const spark_strides_t* sdKp,
+                         const spark_strides_t* sdVp, const spark_strides_t* sdKs, const spark_strides_t* sdVs,
+                         const int* prefix_lens, const int* q_lens, const int* s_lens, void* workspace,
+                         size_t workspace_bytes, int G, int B, int H, int Hkv, int Nq, int P, int S, int d, float scale,
+                         int causal, spark_dtype_t dtype, void* stream) {
+  if (!Q || !O || !LSE || !dO || !dQ || !workspace) return SPARK_ERR_NULL;
+  PrefixProblem p{};
+  PrefixGradArgs a{};
+  int rc = make_prefix(&p, G, B, H, Hkv, Nq, P, S, d, scale, causal, (int)dtype);
+  if (rc != SPARK_OK) return rc;
+  if ((rc = check_part(Q, sQ, B, H, Nq, d, false, &p.mq)) != SPARK_OK) return rc;
+  if ((rc = check_part(Kp, sKp, G, Hkv, P, d, false, &p.mkp)) != SPARK_OK) return rc;
+  if ((rc = check_part(Vp, sVp, G, Hkv, P, d, false, &p.mvp)) != SPARK_OK) return rc;
+  if ((rc = check_part(Ks, sKs, B, Hkv, S, d, false, &p.mks)) != SPARK_OK) return rc;
+  if ((rc = check_part(Vs, sVs, B, Hkv, S, d, false, &p.mvs)) != SPARK_OK) return rc;
+  if ((rc = check_part(O, sO, B, H, Nq, d, false, &p.mo)) != SPARK_OK) return rc;
+  if ((rc = check_part(dO, sdO, B, H, Nq, d, false, &a.mdo)) != SPARK_OK) return rc;
+  if ((rc = check_part(dQ, sdQ, B, H, Nq, d, true, &a.mdq)) != SPARK_OK) return rc;
+  if ((rc = check_part(dKp, sdKp, G, Hkv, P, d, true, &a.mdkp)) != SPARK_OK) return rc;
+  if ((rc = check_part(dVp, sdVp, G, Hkv, P, d, true, &a.mdvp)) != SPARK_OK) return rc;
+  if ((rc = check_part(dKs, sdKs, B, Hkv, S, d, true, &a.mdks)) != SPARK_OK) return rc;
+  if ((rc = check_part(dVs, sdVs, B, Hkv, S, d, true, &a.mdvs)) != SPARK_OK) return rc;
+  if (!aligned16(LSE) || !aligned16(workspace)) return SPARK_ERR_ALIGN;
+  if (workspace_bytes < prefix_bwd_workspace(p)) return SPARK_ERR_WORKSPACE;
+  p.Q = Q; p.Kp = Kp; p.Vp = Vp; p.Ks = Ks; p.Vs = Vs;
+  p.prefix_lens = prefix_lens; p.q_lens = q_lens; p.s_lens = s_lens;
+  a.dO = dO; a.dQ = dQ; a.dKp = dKp; a.dVp = dVp; a.dKs = dKs; a.dVs = dVs; a.LSE = LSE; a.workspace = workspace;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return dtype == SPARK_F16 ? dispatch_prefix_bwd<_Float16>(p, O, a, scale, st)
+                            : dispatch_prefix_bwd<__bf16>(p, O, a, scale, st);
+}
 
 size_t spark_mha_prefix_fwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, spark_dtype_t dtype) {
   PrefixProblem p{};

@@ -3,7 +3,14 @@
 //
 // Softmax over the keys of both parts has one maximum and one sum, so a query tile walks the tiles of the prefix and then
 // those of its suffix in the forward's loop (fwd_kernel.hpp): nothing is merged, and nothing is written but O and LSE.
+//
+// Backward.  P = exp(S - LSE) and D = rowsum(dO o O) belong to a row as a whole, so dS = P o (dP - D) can be formed part by
+// part.  dQ walks both parts as the forward does.  dK and dV of a suffix tile sum over the rows of the heads that share it,
+// those of a prefix tile over the rows of all sequences of the group too: the loop of bwd_dkdv_pipe, whose stages of 64 rows
+// then come from one (sequence, head) after the other.  That sum is long and there are few such tiles: `parts` workgroups
+// share it, each leaves its part in fp32, and a small kernel adds them in their order.
 #pragma once
+#include "bwd_kernels.hpp"
 #include "fwd_kernel.hpp"
 
 namespace spark {
@@ -92,6 +99,267 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
   fwd_tiles<T, D, true, false, NW, PAIR>(static_cast<const T*>(p.Q), head_of<T>(p.Ks, p.mks, x.b, x.hk),
                                          head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, LSE, p.mq, p.mks, p.mvs, p.mo, p.H, p.Nq,
                                          x.S, p.dh, nqt, 0, scale_log2, Dropout{}, keys);
+}
+
+template <typename T> struct PrefixGrads {
+  const T *dO;
+  T *dQ, *dKp, *dVp, *dKs, *dVs;
+  TensorMap mdo, mdq, mdkp, mdvp, mdks, mdvs;
+  const float* LSE;
+  float *Dws, *LSE2ws;  // [B,H,Nq]: -D, LSE * log2(e)
+  float* partial;       // [parts][G * Hkv][P][2][D] of dK / scale and dV, if parts > 1
+  int parts;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void mha_prefix_dq_kernel(PrefixProblem p, const T* __restrict__ O, PrefixGrads<T> gr,
+                                                               int nqt, float scale) {
+  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int flat = logical / nqt, item = logical - flat * nqt;
+  const PrefixHead x(p, flat);
+  const int head = x.b * p.H + x.h;
+  constexpr int BM = BwdQCfg<D, true, false>::BM;
+  const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < p.Nq ? row0 + BM : p.Nq;
+  if (row0 >= x.rows || (x.P == 0 && (x.S == 0 || row1 + x.ahead <= 0))) {  // no row in use, or no key for any
+    zero_rows(gr.dQ + (size_t)x.b * (size_t)gr.mdq.batch + (size_t)x.h * (size_t)gr.mdq.head, gr.mdq, row0, row1, p.dh);
+    for (int i = row0 + threadIdx.x; i < row1; i += 256) {
+      gr.Dws[(size_t)head * p.Nq + i] = 0.f;
+      gr.LSE2ws[(size_t)head * p.Nq + i] = INFINITY;
+    }
+    return;
+  }
+  PrefixAndSuffix<T> keys;
+  keys.head = head;
+  keys.item = item;
+  keys.Kp = head_of<T>(p.Kp, p.mkp, x.grp, x.hk);
+  keys.Vp = head_of<T>(p.Vp, p.mvp, x.grp, x.hk);
+  keys.kp_row_bytes = (uint32_t)p.mkp.row * 2;
+  keys.vp_row_bytes = (uint32_t)p.mvp.row * 2;
+  keys.kp_bytes = span_or_none(p.mkp, x.P, p.dh);
+  keys.vp_bytes = span_or_none(p.mvp, x.P, p.dh);
+  keys.P = x.P;
+  keys.rows = x.rows;
+  keys.ahead = x.ahead;
+  bwd_dq<T, D, true, false, false, IN_ORDER>(static_cast<const T*>(p.Q), head_of<T>(p.Ks, p.mks, x.b, x.hk),
+                                             head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, gr.dO, gr.LSE, gr.Dws, gr.LSE2ws, gr.dQ,
+                                             p.mq, p.mks, p.mvs, p.mo, gr.mdo, gr.mdq, p.H, p.Nq, x.S, p.dh, nqt, 0, scale,
+                                             scale * 1.4426950408889634f, Dropout{}, head, item, keys);
+}
+
+// The query rows that see a key tile, in stages of 64 of one (sequence, head), for bwd_dkdv_pipe; and where its sums go.
+template <typename T, int D> struct GroupRows {
+  static constexpr bool SEVERAL = true;
+  struct Stage {
+    const T *q, *dout;
+    const float *lse2, *dws;
+    uint32_t q_bytes, do_bytes, stat_bytes;
+    int block;
+  };
+  // of the problem, each by itself: a pointer to the kernel's arguments would put them all into scratch memory
+  const T *Q, *dO;
+  const float *lse2, *dws;
+  const int* q_lens;
+  TensorMap mq, mdo;
+  int H, Nq, dh;
+  int b, h, h0, h1, left;  // present pair, the heads of the tile, pairs left with it
+  int k0;                  // causal: the tile's first key, with S keys in the suffix; -1: every row sees the tile
+  int S;
+  int blocks, ahead;       // of the present pair
+  Stage s;
+  T *dK, *dV;              // of the tile's head
+  TensorMap mdk, mdv;
+  int keys, all;           // keys that exist, rows that are written (zeros behind the keys)
+  float* partial;          // or the tile's head's partial sums
+
+  __device__ __forceinline__ Stage stage() const { return s; }
+  __device__ __forceinline__ int first_query() const { return s.block * 64 + ahead; }
+  // Enter the present pair; whether any of its rows sees the tile.
+  __device__ __forceinline__ bool enter() {
+    const int rows = length_of(q_lens, b, Nq);
+    ahead = k0 < 0 ? ALL_AHEAD : S - rows;
+    const int first = k0 < 0 ? 0 : k0 - ahead;  // the first row that sees the tile's first key
+    s.block = first > 0 ? first / 64 : 0;
+    blocks = (rows + 63) / 64;
+    if (s.block >= blocks) return false;
+    const size_t row = ((size_t)b * H + h) * (size_t)Nq;
+    s.q = head_of<T>(Q, mq, b, h);
+    s.dout = head_of<T>(dO, mdo, b, h);
+    s.lse2 = lse2 + row;
+    s.dws = dws + row;
+    s.q_bytes = head_span_bytes(mq, rows, dh);
+    s.do_bytes = head_span_bytes(mdo, rows, dh);
+    s.stat_bytes = (uint32_t)rows * 4;
+    return true;
+  }
+  __device__ __forceinline__ bool next_pair() {
+    while (left > 0) {
+      --left;
+      if (++h == h1) {
+        h = h0;
+        ++b;
+      }
+      if (enter()) return true;
+    }
+    return false;
+  }
+  // The first stage; false if no row sees the tile.
+  __device__ __forceinline__ bool start() { return enter() || next_pair(); }
+  __device__ __forceinline__ bool advance() {
+    if (s.block + 1 < blocks) {
+      ++s.block;
+      return true;
+    }
+    return next_pair();
+  }
+  __device__ __forceinline__ void store(const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32], SPARK_LDS char* ob, int k0w,
+                                        int lane, float scale) const {
+    constexpr int OSTR = BwdKvPipeCfg<D>::OSTR;
+    if (partial) {
+      asm volatile("" : "+v"(lane));
+      const int key = k0w + (lane & 31), g = lane >> 5;
+      float* out = partial + (size_t)key * (2 * D) + 4 * g;
+      if (key >= keys) return;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 a, c;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            a[e] = dk[dt][4 * r4 + e];
+            c[e] = dv[dt][4 * r4 + e];
+          }
+          *reinterpret_cast<f32x4*>(out + dt * 32 + 8 * r4) = a;
+          *reinterpret_cast<f32x4*>(out + D + dt * 32 + 8 * r4) = c;
+        }
+      return;
+    }
+    store_transposed<T, D, OSTR>(dk, scale, ob, dK, k0w, keys, lane, (size_t)mdk.row, dh);
+    store_transposed<T, D, OSTR>(dv, 1.0f, ob, dV, k0w, keys, lane, (size_t)mdv.row, dh);
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(PrefixProblem p, PrefixGrads<T> gr,
+                                                                               int p_tiles, int s_tiles, int first,
+                                                                               float scale) {
+  constexpr int BN = BwdKvPipeCfg<D>::BN;
+  const int per = p.H / p.Hkv, seqs = p.B / p.G;
+  const bool of_prefix = (int)blockIdx.x < first;  // the longer ones first
+  GroupRows<T, D> rows;
+  rows.Q = static_cast<const T*>(p.Q);
+  rows.dO = gr.dO;
+  rows.lse2 = gr.LSE2ws;
+  rows.dws = gr.Dws;
+  rows.q_lens = p.q_lens;
+  rows.mq = p.mq;
+  rows.mdo = gr.mdo;
+  rows.H = p.H;
+  rows.Nq = p.Nq;
+  rows.dh = p.dh;
+  rows.partial = nullptr;
+  int hk, tile;
+  const T *K, *V;
+  TensorMap mk, mv;
+  if (of_prefix) {
+    const int logical = xcd_contiguous(blockIdx.x, first);
+    tile = logical % p_tiles;
+    const int unit = logical / p_tiles, part = unit % gr.parts, owner = unit / gr.parts, grp = owner / p.Hkv;
+    hk = owner - grp * p.Hkv;
+    const int pairs = seqs * per, begin = (int)((int64_t)pairs * part / gr.parts),
+              end = (int)((int64_t)pairs * (part + 1) / gr.parts);
+    rows.b = grp * seqs + begin / per;
+    rows.h0 = hk * per;
+    rows.h = rows.h0 + begin % per;
+    rows.left = end - begin - 1;
+    rows.k0 = -1;
+    rows.S = 0;
+    rows.keys = length_of(p.prefix_lens, grp, p.P);
+    rows.all = p.P;
+    if (gr.parts > 1) rows.partial = gr.partial + ((size_t)part * (size_t)(p.G * p.Hkv) + owner) * (size_t)p.P * (2 * D);
+    rows.dK = gr.dKp + (size_t)grp * (size_t)gr.mdkp.batch + (size_t)hk * (size_t)gr.mdkp.head;
+    rows.dV = gr.dVp + (size_t)grp * (size_t)gr.mdvp.batch + (size_t)hk * (size_t)gr.mdvp.head;
+    rows.mdk = gr.mdkp;
+    rows.mdv = gr.mdvp;
+    K = head_of<T>(p.Kp, p.mkp, grp, hk);
+    V = head_of<T>(p.Vp, p.mvp, grp, hk);
+    mk = p.mkp;
+    mv = p.mvp;
+  } else {
+    const int logical = xcd_contiguous(blockIdx.x - first, gridDim.x - first);
+    tile = logical % s_tiles;
+    const int owner = logical / s_tiles, b = owner / p.Hkv;
+    hk = owner - b * p.Hkv;
+    rows.b = b;
+    rows.h = rows.h0 = hk * per;
+    rows.left = per - 1;
+    rows.keys = rows.S = length_of(p.s_lens, b, p.S);
+    rows.k0 = p.causal ? tile * BN : -1;
+    rows.all = p.S;
+    rows.dK = gr.dKs + (size_t)b * (size_t)gr.mdks.batch + (size_t)hk * (size_t)gr.mdks.head;
+    rows.dV = gr.dVs + (size_t)b * (size_t)gr.mdvs.batch + (size_t)hk * (size_t)gr.mdvs.head;
+    rows.mdk = gr.mdks;
+    rows.mdv = gr.mdvs;
+    K = head_of<T>(p.Ks, p.mks, b, hk);
+    V = head_of<T>(p.Vs, p.mvs, b, hk);
+    mk = p.mks;
+    mv = p.mvs;
+  }
+  rows.h1 = rows.h0 + per;
+  const int k0 = tile * BN, k1 = k0 + BN < rows.all ? k0 + BN : rows.all;
+  const bool none = k0 >= rows.keys || !rows.start();
+  if (!rows.partial) {  // rows of keys that do not exist, or that no query sees
+    const int from = none ? k0 : rows.keys > k0 ? rows.keys : k0;
+    if (from < k1) {
+      zero_rows(rows.dK, rows.mdk, from, k1, p.dh);
+      zero_rows(rows.dV, rows.mdv, from, k1, p.dh);
+    }
+  } else if (none) {
+    const int end = k1 < rows.keys ? k1 : rows.keys;
+    for (int i = threadIdx.x; i < (end - k0) * (2 * D / 4); i += 256)
+      reinterpret_cast<f32x4*>(rows.partial + (size_t)k0 * (2 * D))[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  if (none) return;
+  const TensorMap none_map{0, 0, 0};
+  if (of_prefix)
+    bwd_dkdv_pipe<T, D, false, false, IN_ORDER, false>(nullptr, K, V, nullptr, nullptr, nullptr, nullptr, nullptr, p.mq, mk, mv,
+                                                       gr.mdo, none_map, none_map, 1, p.Nq, rows.keys, p.dh, p_tiles, 0, scale,
+                                                       Dropout{}, 0, tile, rows);
+  else
+    bwd_dkdv_pipe<T, D, true, false, IN_ORDER, false>(nullptr, K, V, nullptr, nullptr, nullptr, nullptr, nullptr, p.mq, mk, mv,
+                                                      gr.mdo, none_map, none_map, 1, p.Nq, rows.keys, p.dh, s_tiles, 0, scale,
+                                                      Dropout{}, 0, tile, rows);
+}
+
+// dKp and dVp from the parts, added in their order: a thread per four columns of a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, float scale) {
+  using v4 = typename Frag<T>::v4;
+  constexpr int LPR = D / 4;
+  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR, owners = (int64_t)p.G * p.Hkv;
+  const int col = (threadIdx.x % LPR) * 4;
+  if (row >= owners * p.P || col >= p.dh) return;
+  const int owner = (int)(row / p.P), key = (int)(row - (int64_t)owner * p.P), grp = owner / p.Hkv, hk = owner - grp * p.Hkv;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
+  if (key < length_of(p.prefix_lens, grp, p.P)) {
+    const float* x = gr.partial + (size_t)row * (2 * D) + col;
+    const size_t step = (size_t)owners * (size_t)p.P * (2 * D);
+#pragma unroll 4
+    for (int i = 0; i < gr.parts; ++i) {
+      a += *reinterpret_cast<const f32x4*>(x + i * step);
+      c += *reinterpret_cast<const f32x4*>(x + i * step + D);
+    }
+  }
+  v4 k, v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    k[e] = (T)(a[e] * scale);
+    v[e] = (T)c[e];
+  }
+  *reinterpret_cast<v4*>(gr.dKp + (size_t)grp * (size_t)gr.mdkp.batch + (size_t)hk * (size_t)gr.mdkp.head +
+                         (size_t)key * (size_t)gr.mdkp.row + col) = k;
+  *reinterpret_cast<v4*>(gr.dVp + (size_t)grp * (size_t)gr.mdvp.batch + (size_t)hk * (size_t)gr.mdvp.head +
+                         (size_t)key * (size_t)gr.mdvp.row + col) = v;
 }
 
 }  // namespace spark

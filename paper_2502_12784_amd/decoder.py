@@ -172,3 +172,33 @@ def spark_mha_prefix_fwd(Q, Kp, Vp, Ks, Vs, scale: float, causal: bool = True, p
                                     LSE.data_ptr(), *strides, *lens, workspace.data_ptr(), nbytes, *sizes, float(scale),
                                     int(bool(causal)), code, _stream_ptr()))
     return O, LSE
+
+
+def spark_mha_prefix_bwd_workspace_bytes(G: int, B: int, H: int, Hkv: int, Nq: int, P: int, S: int, d: int, causal: bool,
+                                         dtype_code: int) -> int:
+    return int(load_library().spark_mha_prefix_bwd_workspace_bytes(G, B, H, Hkv, Nq, P, S, d, int(bool(causal)), dtype_code))
+
+
+def spark_mha_prefix_bwd(Q, Kp, Vp, Ks, Vs, O, LSE, dO, scale: float, causal: bool = True, prefix_lens=None, q_lens=None,
+                         s_lens=None, dQ=None, dKp=None, dVp=None, dKs=None, dVs=None, workspace=None):
+    """dQ, dKp, dVp, dKs, dVs for the problem of spark_mha_prefix_fwd and its O and LSE.  dKp and dVp sum over the sequences
+    that share the prefix; what is not in use is zero.  Gradients default to the layouts of Q, Kp, Vp, Ks, Vs."""
+    import torch
+    lib = load_library()
+    sizes, strides, lens = _prefix_problem(Q, Kp, Vp, Ks, Vs, prefix_lens, q_lens, s_lens)
+    G, B, H, Hkv, Nq, P, S, d = sizes
+    code = _dtype_code(Q)
+    dQ, dKp, dVp, dKs, dVs = (torch.empty_like(like) if t is None else t for t, like in
+                              ((dQ, Q), (dKp, Kp), (dVp, Vp), (dKs, Ks), (dVs, Vs)))
+    _same_device(("O", O), ("LSE", LSE), ("dO", dO), ("dQ", dQ), ("dKp", dKp), ("dVp", dVp), ("dKs", dKs), ("dVs", dVs),
+                 ("workspace", workspace))
+    qs, ps, ss = (B, H, Nq, d), (G, Hkv, P, d), (B, Hkv, S, d)
+    strides += [_rows(t, shape, Q.dtype, n) for t, shape, n in
+                ((O, qs, "O"), (dO, qs, "dO"), (dQ, qs, "dQ"), (dKp, ps, "dKp"), (dVp, ps, "dVp"), (dKs, ss, "dKs"),
+                 (dVs, ss, "dVs"))]
+    binding._require(LSE, (B, H, Nq), torch.float32, "LSE")
+    workspace, nbytes = _scratch(workspace, spark_mha_prefix_bwd_workspace_bytes(*sizes, causal, code), Q)
+    _check(lib.spark_mha_prefix_bwd(*(t.data_ptr() for t in (Q, Kp, Vp, Ks, Vs, O, LSE, dO, dQ, dKp, dVp, dKs, dVs)), *strides,
+                                    *lens, workspace.data_ptr(), nbytes, *sizes, float(scale), int(bool(causal)), code,
+                                    _stream_ptr()))
+    return dQ, dKp, dVp, dKs, dVs
