@@ -61,8 +61,8 @@ template <int D, int NW = 4, bool PAIR = false> struct FwdCfg {
 
 // The keys of a forward's query tile.  One sequence: rows 0 ... Nk-1 of K and V.
 struct OneSequence {
-  static constexpr bool PREFIX = false;
-  static constexpr int head = 0, item = 0, P = 0, rows = 0, ahead = 0;  // not used
+  static constexpr bool PREFIX = false, PACKED = false;
+  static constexpr int head = 0, item = 0, P = 0, rows = 0, ahead = 0, seen = 0;  // not used
   static constexpr uint32_t kp_row_bytes = 0, vp_row_bytes = 0;
   template <typename T>
   __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap& m, int head, int H) const {
@@ -73,7 +73,7 @@ struct OneSequence {
 // them may be empty.  Tiles are walked in this order, so that those without a mask come first: the full tiles of the
 // prefix, the suffix, and the prefix's last tile if it is not full.  (Softmax does not mind the order of the keys.)
 template <typename T> struct PrefixAndSuffix {
-  static constexpr bool PREFIX = true;
+  static constexpr bool PREFIX = true, PACKED = false;
   int head, item;         // the workgroup's: b * H + h, query tile
   const T *Kp, *Vp;       // of this head
   uint32_t kp_row_bytes, vp_row_bytes;
@@ -81,6 +81,21 @@ template <typename T> struct PrefixAndSuffix {
   int P;                  // its keys
   int rows;               // query rows in use, 1 at least; those behind, up to Nq, give zeros and an LSE of -inf
   int ahead;              // query i sees suffix keys j <= i + ahead: causal, or a number that hides none
+  __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap&, int, int) const { return X; }
+};
+
+// A run of one sequence's keys (K, V: its first ones; Nk of them), and query rows that lie anywhere: those of several heads
+// or sequences, packed into one tile.  The tile's results stay unnormalised in fp32, to be merged with those of other runs:
+// a partial result is lds_row<D> + 4 floats, O, then m, l and two unused (16-byte alignment).
+template <typename T> struct PackedRows {
+  static constexpr bool PREFIX = false, PACKED = true;
+  static constexpr int P = 0, rows = 0, ahead = 0;      // not used
+  static constexpr uint32_t kp_row_bytes = 0, vp_row_bytes = 0;
+  int head = 0, item;
+  const T* q;       // this lane's row, any row if it has none
+  float* out;       // its partial result, or nullptr
+  int seen;         // keys of the run that it sees
+  int seen_by_all;  // that all rows of the tile see
   __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap&, int, int) const { return X; }
 };
 
@@ -122,8 +137,8 @@ static __device__ __forceinline__ void fwd_tiles(
   // tail of long tiles.  (With a prefix in front the lengths differ little, and the kernel maps its grid itself.)
   const int items = paired ? causal_items<CAUSAL>(nqt) : nqt;
   const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int head = Keys::PREFIX ? keys.head : logical / items;
-  const int item = Keys::PREFIX ? keys.item : logical - head * items;
+  const int head = Keys::PREFIX || Keys::PACKED ? keys.head : logical / items;
+  const int item = Keys::PREFIX || Keys::PACKED ? keys.item : logical - head * items;
 
   // Nq query rows and Nk key rows per head (equal for self-attention; causal needs them equal)
   const T* Qh = Q + head_base(mq, head, H);
@@ -146,7 +161,17 @@ static __device__ __forceinline__ void fwd_tiles(
     const int qrow_c = qrow < q_end ? qrow : q_end - 1;
 
     v8 qf[KS];
-    load_row_frags(qf, Qh + (size_t)qrow_c * (size_t)mq.row, g, dh);
+    if constexpr (Keys::PACKED) {
+      load_row_frags(qf, keys.q, g, dh);
+      if (!keys.out) {  // a row that is not in use may hold anything
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qf[ks][e] = (T)0.f;
+      }
+    } else {
+      load_row_frags(qf, Qh + (size_t)qrow_c * (size_t)mq.row, g, dh);
+    }
 
     int kv_end = Nk;
     if constexpr (Keys::PREFIX) {
@@ -466,6 +491,22 @@ static __device__ __forceinline__ void fwd_tiles(
       end_round(i);
     }
 
+    if constexpr (Keys::PACKED) {
+      l_run = half_pair_sum(l_run);
+      if (keys.out) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = o[dt][r4 * 4 + e];
+            *reinterpret_cast<f32x4*>(keys.out + dt * 32 + 8 * r4 + 4 * g) = x;
+          }
+        if (g == 0) *reinterpret_cast<f32x4*>(keys.out + lds_row<D>) = f32x4{m_run, l_run, 0.f, 0.f};
+      }
+      return;
+    }
     // Epilogue: normalise, round once, transpose through this wave's LDS slice, store rows.
     // The lane index is read anew: addresses formed from it would otherwise be held in registers across the loop.
     int elane = lane;

@@ -23,13 +23,14 @@
 // against 2048 keys, 128 heads, d = 128: 40.7 -> 29.3 us (4.6 TB/s, the rate of a large copy).
 #pragma once
 #include "dropout_gfx950.hpp"
+#include "fwd_kernel.hpp"
 #include "mma_gfx950.hpp"
 #include "tiles_gfx950.hpp"
 
 namespace spark {
 
-template <int D> struct FwdSplitCfg {
-  static constexpr int NW = 8;                   // waves = key streams of a workgroup
+template <int D, int WAVES = 8> struct FwdSplitCfg {
+  static constexpr int NW = WAVES;               // waves = key streams of a workgroup
   static constexpr int BM = 32;                  // query rows per workgroup
   static constexpr int BN = D == 64 ? 64 : 32;   // keys per tile: 8 KB of K, 8 KB of V
   static constexpr int ROWB = D * 2;
@@ -47,15 +48,15 @@ template <int D> struct FwdSplitCfg {
 
 // PART (not causal): `parts` workgroups share the keys of a query tile; each leaves its m, l and unnormalised
 // O of the rows below Nq in fp32, and mha_fwd_combine_kernel merges them.
-template <typename T, int D, bool CAUSAL, bool DROP, bool PART = false>
-__global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
+template <typename T, int D, bool CAUSAL, bool DROP, bool PART, int WAVES, typename Keys>
+static __device__ __forceinline__ void fwd_split_tiles(
     const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
     float* __restrict__ LSE, TensorMap mq, TensorMap mk, TensorMap mv, TensorMap mo, int H, int Nq, int Nk,
-    int dh, int nqt, int paired, float scale_log2, Dropout dr, int parts, float* __restrict__ partial) {
+    int dh, int nqt, int paired, float scale_log2, Dropout dr, int parts, float* __restrict__ partial, Keys keys) {
   using F = Frag<T>;
   using v8 = typename F::v8;
   using v4 = typename F::v4;
-  using C = FwdSplitCfg<D>;
+  using C = FwdSplitCfg<D, WAVES>;
   constexpr int KS = D / 16, DT = D / 32, HALVES = C::BN / 32;
 
   SPARK_LDS char* const smem = lds_origin();
@@ -71,11 +72,11 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
   const int items = paired ? causal_items<CAUSAL>(nqt) : nqt;
   const int flat = xcd_contiguous(blockIdx.x, gridDim.x);
   const int logical = PART ? flat / parts : flat, part = PART ? flat - logical * parts : 0;
-  const int head = logical / items;
-  const int item = logical - head * items;
+  const int head = Keys::PACKED ? 0 : logical / items;
+  const int item = Keys::PACKED ? 0 : logical - head * items;
 
-  const BufView kview(K + head_base(mk, head, H), head_span_bytes(mk, Nk, dh));
-  const BufView vview(V + head_base(mv, head, H), head_span_bytes(mv, Nk, dh));
+  const BufView kview(keys.head_rows(K, mk, head, H), head_span_bytes(mk, Nk, dh));
+  const BufView vview(keys.head_rows(V, mv, head, H), head_span_bytes(mv, Nk, dh));
   const uint32_t k_row_bytes = (uint32_t)mk.row * 2, v_row_bytes = (uint32_t)mv.row * 2;
   const WaveDma<D> kdma(lane, k_row_bytes, dh), vdma(lane, v_row_bytes, dh);
   const SwzLane<D> off(lane);
@@ -87,13 +88,17 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
       __syncthreads();                  // the first tile's output has left the LDS
     }
     const int q0 = qt * C::BM, qrow = q0 + c32;
-    const T* qp = Q + head_base(mq, head, H) + (size_t)(qrow < Nq ? qrow : Nq - 1) * (size_t)mq.row;
+    const T* qp;
+    if constexpr (Keys::PACKED)
+      qp = keys.q;
+    else
+      qp = Q + head_base(mq, head, H) + (size_t)(qrow < Nq ? qrow : Nq - 1) * (size_t)mq.row;
 
     int kv_end = Nk;
     if (CAUSAL && q0 + C::BM < Nk) kv_end = q0 + C::BM;
     int nt = (kv_end + C::BN - 1) / C::BN;
     int j0 = 0;  // this workgroup's tiles are [j0, nt)
-    if (PART) {
+    if (PART && !Keys::PACKED) {
       const int per = (nt + parts - 1) / parts;
       j0 = part * per;
       nt = j0 + per < nt ? j0 + per : nt;  // the host leaves no part without a tile
@@ -101,9 +106,18 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
     // tiles [0, n_plain) need no mask: they end within the keys and, if causal, at or below row q0
     int n_plain = Nk / C::BN;
     if (CAUSAL && (q0 + 1) / C::BN < n_plain) n_plain = (q0 + 1) / C::BN;
+    if constexpr (Keys::PACKED) n_plain = keys.seen_by_all / C::BN;
 
     v8 qf[KS];
     load_row_frags(qf, qp, g, dh);
+    if constexpr (Keys::PACKED) {
+      if (!keys.out) {  // a row that is not in use may hold anything
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qf[ks][e] = (T)0.f;
+      }
+    }
 
     f32x16 o[DT];
 #pragma unroll
@@ -122,7 +136,7 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));  // Q is awaited here, not in the loop
 
-    const int last_key = (CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;  // as in mha_fwd_kernel
+    const int last_key = (Keys::PACKED ? keys.seen - 1 : CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;  // as in mha_fwd_kernel
     // One tile; next: this wave has another one.  On entry at most NLOAD loads of K and, behind them,
     // NLOAD of V are outstanding.
     auto tile = [&](const int j, auto masked_tag, const bool next) {
@@ -257,6 +271,10 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
       f32x4 sum = lds_read16<f32x4>(smem, q * 1024 + lane * 16);
       for (int w = 1; w < used; ++w) sum += lds_read16<f32x4>(smem, (w * C::GROUPS + q) * 1024 + lane * 16);
       if (PART) {
+        if constexpr (Keys::PACKED) {
+          if (keys.out) *reinterpret_cast<f32x4*>(keys.out + 8 * q + 4 * g) = sum;
+          continue;
+        }
         if (qrow < Nq) *reinterpret_cast<f32x4*>(partial + prow * (D + 4) + 8 * q + 4 * g) = sum;
         continue;
       }
@@ -264,6 +282,10 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
 #pragma unroll
       for (int e = 0; e < 4; ++e) pk[e] = (T)sum[e];
       lds_write(smem + C::STG0, c32 * C::OSTR + (8 * q + 4 * g) * 2, pk);
+    }
+    if constexpr (Keys::PACKED) {
+      if (wave == 0 && g == 0 && keys.out) *reinterpret_cast<f32x4*>(keys.out + D) = f32x4{m_all, l_all, 0.f, 0.f};
+      return;
     }
     if (PART) {
       if (wave == 0 && g == 0 && qrow < Nq) {
@@ -280,6 +302,15 @@ __global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
     if (wave == 0 && g == 0 && qrow < Nq)
       LSE[(size_t)head * Nq + qrow] = (m_all + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
   }  // rep
+}
+
+template <typename T, int D, bool CAUSAL, bool DROP, bool PART = false>
+__global__ __launch_bounds__(512, 1) void mha_fwd_split_kernel(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V, T* __restrict__ O,
+    float* __restrict__ LSE, TensorMap mq, TensorMap mk, TensorMap mv, TensorMap mo, int H, int Nq, int Nk,
+    int dh, int nqt, int paired, float scale_log2, Dropout dr, int parts, float* __restrict__ partial) {
+  fwd_split_tiles<T, D, CAUSAL, DROP, PART, 8>(Q, K, V, O, LSE, mq, mk, mv, mo, H, Nq, Nk, dh, nqt, paired, scale_log2, dr,
+                                               parts, partial, OneSequence{});
 }
 
 // Merge of the partial results of a row (Eq. 3): D / 4 lanes per row.  A partial result is D + 4 floats: O, m,

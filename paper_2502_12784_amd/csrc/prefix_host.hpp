@@ -2,6 +2,7 @@
 #pragma once
 #include "host_util.hpp"
 #include "prefix_kernels.hpp"
+#include "prefix_parts.hpp"
 
 namespace {
 
@@ -45,8 +46,60 @@ int launch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, float scale, 
   return launch_ok("forward kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
+// Whether the rows are packed and the keys go to several workgroups in runs (prefix_parts.hpp).
+bool prefix_packed(const PrefixProblem& p) {
+  return p.Nq <= 32 || (int64_t)p.B * p.H * ((p.Nq + 127) / 128) < 256;
+}
+PrefixParts prefix_runs(const PrefixProblem& p) {
+  PrefixParts s{};
+  const int64_t per = p.H / p.Hkv, rows = (int64_t)(p.B / p.G) * p.Nq * per;
+  const int bn = p.dh <= 64 ? 64 : 32;
+  s.wide = rows > 32;
+  s.p_tiles = p.P ? (int)((rows + (s.wide ? 127 : 31)) / (s.wide ? 128 : 32)) : 0;
+  s.s_tiles = p.S ? (int)((p.Nq * per + 31) / 32) : 0;
+  const int64_t n1 = (int64_t)p.G * p.Hkv * s.p_tiles, n2 = (int64_t)p.B * p.Hkv * s.s_tiles;
+  auto runs = [](int64_t units, int64_t items, int64_t most) {
+    int64_t n = items ? 256 / items : 0;
+    if (n > units) n = units;
+    if (n > most) n = most;
+    return (int)(n < 1 ? 1 : n);
+  };
+  // at least four tiles of the wide loop to a run, or two rounds of the four key streams
+  s.p_parts = p.P ? runs(s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn), n1, 64) : 0;
+  s.s_parts = p.S ? runs((p.S + 8 * bn - 1) / (8 * bn), n2, 16) : 0;
+  s.p_items = (int)(n1 * s.p_parts);
+  return s;
+}
+size_t prefix_fwd_workspace(const PrefixProblem& p) {
+  if (!prefix_packed(p)) return 0;
+  const PrefixParts s = prefix_runs(p);
+  return (size_t)p.B * p.H * p.Nq * (size_t)(s.p_parts + s.s_parts) * ((p.dh <= 64 ? 64 : 128) + 4) * sizeof(float);
+}
+
+template <typename T, int D>
+int launch_prefix_parts(const PrefixProblem& p, void* O, float* LSE, void* workspace, float scale, hipStream_t st) {
+  constexpr int W = lds_row<D>, SMEM = FwdCfg<D>::SMEM > FwdSplitCfg<W, 4>::SMEM ? FwdCfg<D>::SMEM : FwdSplitCfg<W, 4>::SMEM;
+  auto kernel = mha_prefix_parts_kernel<T, D>;
+  static std::atomic<uint64_t> ready{0};
+  const int attr = ensure_smem(kernel, SMEM, ready);
+  if (attr != SPARK_OK) return attr;
+  PrefixParts s = prefix_runs(p);
+  s.partial = static_cast<float*>(workspace);
+  const int grid = s.p_items + p.B * p.Hkv * s.s_tiles * s.s_parts;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), SMEM, st, p, s, scale * 1.4426950408889634f);
+  if (!launch_ok("forward kernel (prefix, in runs)")) return SPARK_ERR_LAUNCH;
+  hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W>), dim3((unsigned)(p.B * p.H * p.Nq)), dim3(256), 0, st, p, s.partial,
+                     s.p_parts + s.s_parts, static_cast<T*>(O), LSE);
+  return launch_ok("forward merge kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
+}
+
 template <typename T>
-int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, float scale, hipStream_t st) {
+int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, void* workspace, float scale, hipStream_t st) {
+  if (workspace && prefix_packed(p)) {
+    if (p.dh <= 64) return launch_prefix_parts<T, 64>(p, O, LSE, workspace, scale, st);
+    if (p.dh <= 96) return launch_prefix_parts<T, 96>(p, O, LSE, workspace, scale, st);
+    return launch_prefix_parts<T, 128>(p, O, LSE, workspace, scale, st);
+  }
   if (p.dh <= 64) return launch_prefix_fwd<T, 64, 4, false>(p, O, LSE, scale, st);
   if (p.dh <= 96) return launch_prefix_fwd<T, 96, 4, false>(p, O, LSE, scale, st);
   return launch_prefix_fwd<T, 128, 4, false>(p, O, LSE, scale, st);
@@ -180,7 +233,7 @@ int spark_mha_prefix_bwd(const void* Q, const void* Kp, const void* Vp, const vo
 size_t spark_mha_prefix_fwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, spark_dtype_t dtype) {
   PrefixProblem p{};
   if (make_prefix(&p, G, B, H, Hkv, Nq, P, S, d, 1.0f, 0, (int)dtype) != SPARK_OK) return 0;
-  return 0;
+  return prefix_fwd_workspace(p);
 }
 
 int spark_mha_prefix_fwd(const void* Q, const void* Kp, const void* Vp, const void* Ks, const void* Vs, void* O, float* LSE,
@@ -200,11 +253,12 @@ int spark_mha_prefix_fwd(const void* Q, const void* Kp, const void* Vp, const vo
   if ((rc = check_part(Vs, sVs, B, Hkv, S, d, false, &p.mvs)) != SPARK_OK) return rc;
   if ((rc = check_part(O, sO, B, H, Nq, d, true, &p.mo)) != SPARK_OK) return rc;
   if (!aligned16(LSE) || !aligned16(workspace)) return SPARK_ERR_ALIGN;
+  if (workspace && workspace_bytes < prefix_fwd_workspace(p)) return SPARK_ERR_WORKSPACE;
   p.Q = Q; p.Kp = Kp; p.Vp = Vp; p.Ks = Ks; p.Vs = Vs;
   p.prefix_lens = prefix_lens; p.q_lens = q_lens; p.s_lens = s_lens;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return dtype == SPARK_F16 ? dispatch_prefix_fwd<_Float16>(p, O, LSE, scale, st)
-                            : dispatch_prefix_fwd<__bf16>(p, O, LSE, scale, st);
+  return dtype == SPARK_F16 ? dispatch_prefix_fwd<_Float16>(p, O, LSE, workspace, scale, st)
+                            : dispatch_prefix_fwd<__bf16>(p, O, LSE, workspace, scale, st);
 }
 
 }  // extern "C"

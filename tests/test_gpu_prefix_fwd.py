@@ -57,9 +57,10 @@ def check(G, B, H, Hkv, Nq, P, S, d, dtype, causal=True, pl=None, ql=None, sl=No
                 t[b, :, max(0, min(m, n)):] = float("nan") if t is not x[4] else float("inf")
     pl, ql, sl = ints(pl), ints(ql), ints(sl)
     scale = d ** -0.5
-    got = spark_mha_prefix_fwd(*x, scale, causal, pl, ql, sl)
-    torch.cuda.synchronize()
-    check_fwd(x, scale, causal, pl, ql, sl, got, dtype)
+    for workspace in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):  # what the call asks for; none
+        got = spark_mha_prefix_fwd(*x, scale, causal, pl, ql, sl, workspace=workspace)
+        torch.cuda.synchronize()
+        check_fwd(x, scale, causal, pl, ql, sl, got, dtype)
     return x, got
 
 
