@@ -244,6 +244,304 @@ PyObject* host_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- the operators around a decoder's attention ----
+
+// The current device and its stream; false with a Python error set if torch cannot say.
+struct Here {
+  void* stream;
+  long device;
+};
+bool here(Here* h) {
+  PyObject* dev = PyObject_CallNoArgs(get_device);
+  if (!dev) return false;
+  h->device = PyLong_AsLong(dev);
+  PyObject* raw = PyObject_CallOneArg(get_raw_stream, dev);
+  Py_DECREF(dev);
+  if (!raw) return false;
+  h->stream = PyLong_AsVoidPtr(raw);
+  Py_DECREF(raw);
+  return !PyErr_Occurred();
+}
+
+// Arguments of one call as they are checked: everything ordinary, on the current device, so far.
+class Arguments {
+ public:
+  explicit Arguments(long device) : device_(device) {}
+  bool ok = true;
+  // a tensor of this rank, or nullptr
+  const at::Tensor* tensor(PyObject* o, int rank) {
+    const at::Tensor* t = plain(o, rank);
+    if (!t || t->device().index() != device_) ok = false;
+    return ok ? t : nullptr;
+  }
+  const at::Tensor* view(PyObject* o, at::ScalarType st, int64_t a, int64_t b, int64_t n, int64_t d) {
+    const at::Tensor* t = tensor(o, 4);
+    if (ok && !(t->scalar_type() == st && t->size(0) == a && t->size(1) == b && t->size(2) == n && t->size(3) == d &&
+                t->stride(3) == 1))
+      ok = false;
+    return ok ? t : nullptr;
+  }
+  const at::Tensor* dense(PyObject* o, at::ScalarType st, at::IntArrayRef sizes) {
+    const at::Tensor* t = tensor(o, (int)sizes.size());
+    if (ok && !(t->scalar_type() == st && t->sizes() == sizes && t->is_contiguous())) ok = false;
+    return ok ? t : nullptr;
+  }
+  const at::Tensor* given(PyObject* o, at::ScalarType st, int64_t a, int64_t b, int64_t n, int64_t d) {
+    return o == Py_None ? nullptr : view(o, st, a, b, n, d);
+  }
+  // address of an optional [a] or [a, b] tensor of int32
+  const int* lengths(PyObject* o, at::IntArrayRef sizes) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor* t = dense(o, at::kInt, sizes);
+    return ok ? static_cast<const int*>(t->data_ptr()) : nullptr;
+  }
+
+ private:
+  const long device_;
+};
+spark_strides_t of(const at::Tensor& t) { return spark_strides_t{t.stride(0), t.stride(1), t.stride(2)}; }
+bool fits(const at::Tensor& t) {
+  for (int i = 0; i < (int)t.dim(); ++i)
+    if (t.size(i) > INT_MAX) return false;
+  return true;
+}
+PyObject* result(std::initializer_list<at::Tensor> list) {
+  PyObject* out = PyTuple_New((Py_ssize_t)list.size());
+  if (!out) return nullptr;
+  Py_ssize_t i = 0;
+  for (const at::Tensor& t : list) PyTuple_SET_ITEM(out, i++, THPVariable_Wrap(t));
+  return out;
+}
+bool half_type(at::ScalarType st) { return st == at::kHalf || st == at::kBFloat16; }
+
+// What both directions of the norm and rotation share: Q, K, wq | None, wk | None, cos | None, sin | None,
+// positions | None, eps, interleaved (in two places of the argument list).
+struct QkCall {
+  const at::Tensor *Q, *K;
+  const void *wq = nullptr, *wk = nullptr;
+  const float *cos = nullptr, *sin = nullptr;
+  const int* positions;
+  at::ScalarType st;
+  spark_dtype_t code;
+  int B, H, N, d, Hkv, rd = 0, table = 0, fp32 = 0, interleaved;
+  float eps;
+};
+bool qk_call(Arguments& args, PyObject* const* a, PyObject* positions, PyObject* eps, PyObject* interleaved, QkCall* c) {
+  if (!PyFloat_Check(eps) || !PyBool_Check(interleaved)) return false;
+  c->Q = args.tensor(a[0], 4);
+  c->K = args.tensor(a[1], 4);
+  if (!args.ok || !fits(*c->Q) || !fits(*c->K) || !half_type(c->Q->scalar_type())) return false;
+  c->st = c->Q->scalar_type();
+  c->code = c->st == at::kHalf ? SPARK_F16 : SPARK_BF16;
+  c->B = (int)c->Q->size(0); c->H = (int)c->Q->size(1); c->N = (int)c->Q->size(2); c->d = (int)c->Q->size(3);
+  c->Hkv = (int)c->K->size(1);
+  args.view(a[0], c->st, c->B, c->H, c->N, c->d);
+  args.view(a[1], c->st, c->B, c->Hkv, c->N, c->d);
+  const at::ScalarType wt[2] = {at::kFloat, c->st};
+  at::ScalarType seen = at::kFloat;
+  for (int i = 0; i < 2 && args.ok; ++i) {
+    if (a[2 + i] == Py_None) continue;
+    const at::Tensor* w = args.tensor(a[2 + i], 1);
+    if (!args.ok || w->size(0) != c->d || !w->is_contiguous()) return false;
+    if (w->scalar_type() != wt[0] && w->scalar_type() != wt[1]) return false;
+    if ((c->wq || c->wk) && w->scalar_type() != seen) return false;
+    seen = w->scalar_type();
+    c->fp32 = seen == at::kFloat;
+    (i ? c->wk : c->wq) = w->data_ptr();
+  }
+  if (!args.ok || (a[4] == Py_None) != (a[5] == Py_None)) return false;
+  if (a[4] != Py_None) {
+    const at::Tensor *x = args.tensor(a[4], 2), *y = args.tensor(a[5], 2);
+    if (!args.ok || x->scalar_type() != at::kFloat || y->scalar_type() != at::kFloat || !x->is_contiguous() ||
+        !y->is_contiguous() || x->sizes() != y->sizes() || !fits(*x) || x->size(1) > 64)
+      return false;
+    c->table = (int)x->size(0);
+    c->rd = 2 * (int)x->size(1);
+    c->cos = static_cast<const float*>(x->data_ptr());
+    c->sin = static_cast<const float*>(y->data_ptr());
+  }
+  c->positions = args.lengths(positions, {c->B, c->N});
+  c->eps = (float)PyFloat_AS_DOUBLE(eps);
+  c->interleaved = interleaved == Py_True;
+  return args.ok;
+}
+
+// qk_fwd(Q, K, wq, wk, cos, sin, positions, eps, interleaved, Qr | None, Kr | None)
+PyObject* host_qk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Here h;
+  QkCall c;
+  if (n != 11 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (!here(&h)) return nullptr;
+  Arguments args(h.device);
+  if (!qk_call(args, a, a[6], a[7], a[8], &c)) Py_RETURN_NONE;
+  const at::Tensor *Qr = args.given(a[9], c.st, c.B, c.H, c.N, c.d), *Kr = args.given(a[10], c.st, c.B, c.Hkv, c.N, c.d);
+  if (!args.ok) Py_RETURN_NONE;
+  const Allocator fresh(*c.Q);
+  const at::Tensor q = Qr ? *Qr : fresh.same(*c.Q), k = Kr ? *Kr : fresh.same(*c.K);
+  void *qp = q.data_ptr(), *kp = k.data_ptr();
+  const void *Qp = c.Q->data_ptr(), *Kp = c.K->data_ptr();
+  const spark_strides_t sQ = of(*c.Q), sK = of(*c.K), sq = of(q), sk = of(k);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS;
+  rc = spark_qk_norm_rope_fwd(Qp, Kp, c.wq, c.wk, c.cos, c.sin, c.positions, qp, kp, &sQ, &sK, &sq, &sk, c.B, c.N, c.H, c.Hkv,
+                              c.d, c.rd, c.table, c.eps, c.interleaved, c.fp32, c.code, h.stream);
+  Py_END_ALLOW_THREADS;
+  if (rc != SPARK_OK) return PyLong_FromLong(rc);
+  return result({q, k});
+  END_HANDLE_TH_ERRORS
+}
+
+// qk_bwd(Q, K, wq, wk, cos, sin, dQr, dKr, positions, eps, interleaved, dQ | None, dK | None, dwq | None, dwk | None)
+PyObject* host_qk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Here h;
+  QkCall c;
+  if (n != 15 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (!here(&h)) return nullptr;
+  Arguments args(h.device);
+  if (!qk_call(args, a, a[8], a[9], a[10], &c)) Py_RETURN_NONE;
+  const at::Tensor *gq = args.view(a[6], c.st, c.B, c.H, c.N, c.d), *gk = args.view(a[7], c.st, c.B, c.Hkv, c.N, c.d);
+  const at::Tensor *dQg = args.given(a[11], c.st, c.B, c.H, c.N, c.d), *dKg = args.given(a[12], c.st, c.B, c.Hkv, c.N, c.d);
+  const at::Tensor* dwg[2];
+  for (int i = 0; i < 2; ++i) dwg[i] = a[13 + i] == Py_None ? nullptr : args.dense(a[13 + i], at::kFloat, {c.d});
+  if (!args.ok) Py_RETURN_NONE;
+  const Allocator fresh(*c.Q);
+  const at::Tensor dQ = dQg ? *dQg : fresh.same(*c.Q), dK = dKg ? *dKg : fresh.same(*c.K);
+  const at::Tensor dwq = dwg[0] ? *dwg[0] : fresh.contiguous({c.d}, at::kFloat),
+                   dwk = dwg[1] ? *dwg[1] : fresh.contiguous({c.d}, at::kFloat);
+  const size_t need = spark_qk_norm_rope_bwd_workspace_bytes(c.B, c.N, c.H, c.Hkv, c.d, c.rd, c.code);
+  const at::Tensor ws = fresh.contiguous({(int64_t)(need > 16 ? need : 16)}, at::kByte);
+  const void *Qp = c.Q->data_ptr(), *Kp = c.K->data_ptr(), *gqp = gq->data_ptr(), *gkp = gk->data_ptr();
+  void *dQp = dQ.data_ptr(), *dKp = dK.data_ptr(), *wsp = ws.data_ptr();
+  float *dwqp = static_cast<float*>(dwq.data_ptr()), *dwkp = static_cast<float*>(dwk.data_ptr());
+  const spark_strides_t sQ = of(*c.Q), sK = of(*c.K), sgq = of(*gq), sgk = of(*gk), sdq = of(dQ), sdk = of(dK);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS;
+  rc = spark_qk_norm_rope_bwd(Qp, Kp, c.wq, c.wk, c.cos, c.sin, c.positions, gqp, gkp, dQp, dKp, dwqp, dwkp, &sQ, &sK, &sgq,
+                              &sgk, &sdq, &sdk, wsp, need, c.B, c.N, c.H, c.Hkv, c.d, c.rd, c.table, c.eps, c.interleaved,
+                              c.fp32, c.code, h.stream);
+  Py_END_ALLOW_THREADS;
+  if (rc != SPARK_OK) return PyLong_FromLong(rc);
+  return result({dQ, dK, dwq, dwk});
+  END_HANDLE_TH_ERRORS
+}
+
+// What both directions of the attention behind a prefix share.
+struct PrefixCall {
+  const at::Tensor* x[5];  // Q, Kp, Vp, Ks, Vs
+  at::ScalarType st;
+  spark_dtype_t code;
+  int G, B, H, Hkv, Nq, P, S, d, causal;
+  float scale;
+  const int *prefix_lens, *q_lens, *s_lens;
+  spark_strides_t s[5];
+  const void* p[5];
+};
+// x: Q, Kp, Vp, Ks, Vs;  how: scale, causal, prefix_lens | None, q_lens | None, s_lens | None
+bool prefix_call(Arguments& args, PyObject* const* x, PyObject* const* how, PrefixCall* c) {
+  if (!PyFloat_Check(how[0]) || !PyBool_Check(how[1])) return false;
+  for (int i = 0; i < 5; ++i) {
+    c->x[i] = args.tensor(x[i], 4);
+    if (!args.ok || !fits(*c->x[i])) return false;
+  }
+  c->st = c->x[0]->scalar_type();
+  if (!half_type(c->st)) return false;
+  c->code = c->st == at::kHalf ? SPARK_F16 : SPARK_BF16;
+  c->B = (int)c->x[0]->size(0); c->H = (int)c->x[0]->size(1); c->Nq = (int)c->x[0]->size(2); c->d = (int)c->x[0]->size(3);
+  c->G = (int)c->x[1]->size(0); c->Hkv = (int)c->x[1]->size(1); c->P = (int)c->x[1]->size(2); c->S = (int)c->x[3]->size(2);
+  args.view(x[0], c->st, c->B, c->H, c->Nq, c->d);
+  args.view(x[1], c->st, c->G, c->Hkv, c->P, c->d);
+  args.view(x[2], c->st, c->G, c->Hkv, c->P, c->d);
+  args.view(x[3], c->st, c->B, c->Hkv, c->S, c->d);
+  args.view(x[4], c->st, c->B, c->Hkv, c->S, c->d);
+  c->prefix_lens = args.lengths(how[2], {c->G});
+  c->q_lens = args.lengths(how[3], {c->B});
+  c->s_lens = args.lengths(how[4], {c->B});
+  if (!args.ok) return false;
+  c->scale = (float)PyFloat_AS_DOUBLE(how[0]);
+  c->causal = how[1] == Py_True;
+  for (int i = 0; i < 5; ++i) {
+    c->s[i] = of(*c->x[i]);
+    c->p[i] = c->x[i]->data_ptr();
+  }
+  return true;
+}
+
+// prefix_fwd(Q, Kp, Vp, Ks, Vs, scale, causal, prefix_lens, q_lens, s_lens, O | None, LSE | None)
+PyObject* host_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Here h;
+  PrefixCall c;
+  if (n != 12 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (!here(&h)) return nullptr;
+  Arguments args(h.device);
+  if (!prefix_call(args, a, a + 5, &c)) Py_RETURN_NONE;
+  const at::Tensor* Og = args.given(a[10], c.st, c.B, c.H, c.Nq, c.d);
+  const at::Tensor* Lg = a[11] == Py_None ? nullptr : args.dense(a[11], at::kFloat, {c.B, c.H, c.Nq});
+  if (!args.ok) Py_RETURN_NONE;
+  const Allocator fresh(*c.x[0]);
+  const at::Tensor O = Og ? *Og : fresh.same(*c.x[0]), L = Lg ? *Lg : fresh.contiguous({c.B, c.H, c.Nq}, at::kFloat);
+  const size_t need = spark_mha_prefix_fwd_workspace_bytes(c.G, c.B, c.H, c.Hkv, c.Nq, c.P, c.S, c.d, c.code);
+  at::Tensor ws;
+  if (need) ws = fresh.contiguous({(int64_t)need}, at::kByte);
+  void *o = O.data_ptr(), *wsp = need ? ws.data_ptr() : nullptr;
+  float* lse = static_cast<float*>(L.data_ptr());
+  const spark_strides_t sO = of(O);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS;
+  rc = spark_mha_prefix_fwd(c.p[0], c.p[1], c.p[2], c.p[3], c.p[4], o, lse, &c.s[0], &c.s[1], &c.s[2], &c.s[3], &c.s[4], &sO,
+                            c.prefix_lens, c.q_lens, c.s_lens, wsp, need, c.G, c.B, c.H, c.Hkv, c.Nq, c.P, c.S, c.d, c.scale,
+                            c.causal, c.code, h.stream);
+  Py_END_ALLOW_THREADS;
+  if (rc != SPARK_OK) return PyLong_FromLong(rc);
+  return result({O, L});
+  END_HANDLE_TH_ERRORS
+}
+
+// prefix_bwd(Q, Kp, Vp, Ks, Vs, O, LSE, dO, scale, causal, prefix_lens, q_lens, s_lens, dQ | None, dKp | None, dVp | None,
+//            dKs | None, dVs | None)
+PyObject* host_prefix_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Here h;
+  PrefixCall c;
+  if (n != 18 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (!here(&h)) return nullptr;
+  Arguments args(h.device);
+  if (!prefix_call(args, a, a + 8, &c)) Py_RETURN_NONE;
+  const at::Tensor *O = args.view(a[5], c.st, c.B, c.H, c.Nq, c.d), *dO = args.view(a[7], c.st, c.B, c.H, c.Nq, c.d);
+  const at::Tensor* L = args.dense(a[6], at::kFloat, {c.B, c.H, c.Nq});
+  const at::Tensor* given[5];
+  for (int i = 0; i < 5; ++i)
+    given[i] = !args.ok ? nullptr : args.given(a[13 + i], c.st, c.x[i]->size(0), c.x[i]->size(1), c.x[i]->size(2), c.d);
+  if (!args.ok) Py_RETURN_NONE;
+  const Allocator fresh(*c.x[0]);
+  at::Tensor g[5];
+  void* gp[5];
+  spark_strides_t gs[5];
+  for (int i = 0; i < 5; ++i) {
+    g[i] = given[i] ? *given[i] : fresh.same(*c.x[i]);
+    gp[i] = g[i].data_ptr();
+    gs[i] = of(g[i]);
+  }
+  const size_t need = spark_mha_prefix_bwd_workspace_bytes(c.G, c.B, c.H, c.Hkv, c.Nq, c.P, c.S, c.d, c.causal, c.code);
+  const at::Tensor ws = fresh.contiguous({(int64_t)(need > 16 ? need : 16)}, at::kByte);
+  const void *o = O->data_ptr(), *dout = dO->data_ptr();
+  const float* lse = static_cast<const float*>(L->data_ptr());
+  void* wsp = ws.data_ptr();
+  const spark_strides_t sO = of(*O), sdO = of(*dO);
+  int rc;
+  Py_BEGIN_ALLOW_THREADS;
+  rc = spark_mha_prefix_bwd(c.p[0], c.p[1], c.p[2], c.p[3], c.p[4], o, lse, dout, gp[0], gp[1], gp[2], gp[3], gp[4], &c.s[0],
+                            &c.s[1], &c.s[2], &c.s[3], &c.s[4], &sO, &sdO, &gs[0], &gs[1], &gs[2], &gs[3], &gs[4],
+                            c.prefix_lens, c.q_lens, c.s_lens, wsp, need, c.G, c.B, c.H, c.Hkv, c.Nq, c.P, c.S, c.d, c.scale,
+                            c.causal, c.code, h.stream);
+  Py_END_ALLOW_THREADS;
+  if (rc != SPARK_OK) return PyLong_FromLong(rc);
+  return result({g[0], g[1], g[2], g[3], g[4]});
+  END_HANDLE_TH_ERRORS
+}
+
 // bind(get_device, get_raw_stream)
 PyObject* host_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 2 || !PyCallable_Check(a[0]) || !PyCallable_Check(a[1])) {
@@ -262,6 +560,10 @@ PyMethodDef methods[] = {
     {"bind", SPARK_FASTCALL(host_bind), "the two torch functions that name the current stream"},
     {"fwd", SPARK_FASTCALL(host_fwd), "forward"},
     {"bwd", SPARK_FASTCALL(host_bwd), "backward"},
+    {"qk_fwd", SPARK_FASTCALL(host_qk_fwd), "norm and rotation of queries and keys"},
+    {"qk_bwd", SPARK_FASTCALL(host_qk_bwd), "its backward"},
+    {"prefix_fwd", SPARK_FASTCALL(host_prefix_fwd), "attention behind a shared prefix"},
+    {"prefix_bwd", SPARK_FASTCALL(host_prefix_bwd), "its backward"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_spark_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,11 +1,12 @@
 """The operators around a decoder's attention: norm and rotation of queries and keys, attention behind a shared prefix.
 
-Argument marshalling only, as in ``binding``: the work is done by the HIP kernels of ``libspark_mha.so``.
+Argument marshalling only, as in ``binding``: the work is done by the HIP kernels of ``libspark_mha.so``.  Ordinary calls are
+marshalled by the extension ``_spark_host``; what it does not take (and every error) goes through the code here.
 """
 from __future__ import annotations
 
 from . import binding
-from .binding import Strides, _check, _dtype_code, _stream_ptr, load_library
+from .binding import Strides, _check, _dtype_code, _native, _stream_ptr, load_library
 
 
 def _same_device(*tensors):
@@ -86,6 +87,9 @@ def spark_qk_norm_rope_fwd(Q, K, wq, wk, cos, sin, positions=None, eps: float = 
     padding, whose results are zeros.  Any strides; Qr and Kr may be given, as Q and K themselves or as rows of a cache."""
     import torch
     lib = load_library()
+    out = binding._host.qk_fwd(Q, K, wq, wk, cos, sin, positions, eps, interleaved, Qr, Kr)
+    if out is not None:
+        return _native(out)
     address, sizes = _qk_problem(Q, K, wq, wk, cos, sin, positions, eps, interleaved)
     B, N, H, Hkv, d = sizes[:5]
     Qr = torch.empty_like(Q) if Qr is None else Qr
@@ -108,6 +112,10 @@ def spark_qk_norm_rope_bwd(Q, K, wq, wk, cos, sin, dQr, dKr, positions=None, eps
     dwq and dwk are fp32."""
     import torch
     lib = load_library()
+    if workspace is None:
+        out = binding._host.qk_bwd(Q, K, wq, wk, cos, sin, dQr, dKr, positions, eps, interleaved, dQ, dK, dwq, dwk)
+        if out is not None:
+            return _native(out)
     address, sizes = _qk_problem(Q, K, wq, wk, cos, sin, positions, eps, interleaved)
     B, N, H, Hkv, d, rd = sizes[:6]
     dQ = torch.empty_like(Q) if dQ is None else dQ
@@ -160,6 +168,10 @@ def spark_mha_prefix_fwd(Q, Kp, Vp, Ks, Vs, scale: float, causal: bool = True, p
     workgroup's, which for few rows is slow."""
     import torch
     lib = load_library()
+    if workspace is None:
+        out = binding._host.prefix_fwd(Q, Kp, Vp, Ks, Vs, scale, causal, prefix_lens, q_lens, s_lens, O, LSE)
+        if out is not None:
+            return _native(out)
     sizes, strides, lens = _prefix_problem(Q, Kp, Vp, Ks, Vs, prefix_lens, q_lens, s_lens)
     G, B, H, Hkv, Nq, P, S, d = sizes
     code = _dtype_code(Q)
@@ -186,6 +198,11 @@ def spark_mha_prefix_bwd(Q, Kp, Vp, Ks, Vs, O, LSE, dO, scale: float, causal: bo
     that share the prefix; what is not in use is zero.  Gradients default to the layouts of Q, Kp, Vp, Ks, Vs."""
     import torch
     lib = load_library()
+    if workspace is None:
+        out = binding._host.prefix_bwd(Q, Kp, Vp, Ks, Vs, O, LSE, dO, scale, causal, prefix_lens, q_lens, s_lens, dQ, dKp, dVp,
+                                       dKs, dVs)
+        if out is not None:
+            return _native(out)
     sizes, strides, lens = _prefix_problem(Q, Kp, Vp, Ks, Vs, prefix_lens, q_lens, s_lens)
     G, B, H, Hkv, Nq, P, S, d = sizes
     code = _dtype_code(Q)

@@ -152,3 +152,23 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, held))
+
+
+def test_general_path_of_the_binding_gives_the_same():
+    """A call that the native path leaves to the Python one (a tensor subclass), forward and backward, both operators."""
+    from paper_2502_12784_amd import spark_qk_norm_rope_bwd, spark_qk_norm_rope_fwd
+    x = make(2, 4, 4, 2, 33, 70, 33, 64, BF16, 12)
+    dO = make(1, 4, 4, 1, 33, 1, 1, 64, BF16, 13)[0]
+    lens = [ints([70, 9]), ints([33, 1, 0, 20]), ints([30, 1, 2, 33])]
+    a = step(x, dO, 0.125, True, lens)
+    y = [torch.nn.Parameter(x[0], requires_grad=False)] + list(x[1:])
+    b = step(y, dO, 0.125, True, lens)
+    for s, t in zip(a, b):
+        assert all(torch.equal(u, v) for u, v in zip(s, t))
+    w = torch.ones(64, device="cuda")
+    cos, sin = du.tables(33, 64)
+    for Q in (x[0], y[0]):
+        got = (*spark_qk_norm_rope_fwd(Q, x[3], w, w, cos, sin),
+               *spark_qk_norm_rope_bwd(Q, x[3], w, w, cos, sin, dO, x[4]))
+        want = got if Q is x[0] else want  # noqa: F821
+        assert all(torch.equal(u, v) for u, v in zip(got, want))
