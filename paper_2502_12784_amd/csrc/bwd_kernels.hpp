@@ -635,7 +635,11 @@ static __device__ __forceinline__ void bwd_dq(
     const int qrow_c = qrow < q_end ? qrow : q_end - 1;
 
     v8 qf[KS], dof[KS], of[KS];  // of: the row of O, needed for D only
-    if constexpr (CAUSAL) {
+    if constexpr (Keys::PREFIX) {
+      load_row_frags(qf, Q + keys.offset(mq, qrow_c), g, dh);
+      load_row_frags(dof, dO + keys.offset(mdo, qrow_c), g, dh);
+      load_row_frags(of, O + keys.offset(mo, qrow_c), g, dh);
+    } else if constexpr (CAUSAL) {
       load_row_frags(qf, Qh + (size_t)qrow_c * (size_t)mq.row, g, dh);
       load_row_frags(dof, dOh + (size_t)qrow_c * (size_t)mdo.row, g, dh);
       if constexpr (!STATS) load_row_frags(of, Oh + (size_t)qrow_c * (size_t)mo.row, g, dh);
@@ -645,12 +649,14 @@ static __device__ __forceinline__ void bwd_dq(
       if constexpr (!STATS)
         load_row_frags(of, BufView(Oh, head_span_bytes(mo, Nq, dh)), (uint32_t)qrow_c * ((uint32_t)mo.row * 2), g, dh);
     }
-    float lse2 = STATS ? LSE2ws[(size_t)head * Nq + qrow_c] : LSE[(size_t)head * Nq + qrow_c];
-    float Dq = STATS ? -Dws[(size_t)head * Nq + qrow_c] : 0.f;
+    size_t stat = (size_t)head * Nq + qrow_c;  // this row's place in the statistics
+    if constexpr (Keys::PREFIX) stat = keys.stat(qrow_c);
+    float lse2 = STATS ? LSE2ws[stat] : LSE[stat];
+    float Dq = STATS ? -Dws[stat] : 0.f;
 
     int kv_end = Nk;
     if constexpr (Keys::PREFIX) {
-      const int lim = (qt + 1) * C::BM + keys.ahead;
+      const int lim = ((qt + 1) * C::BM - 1) / keys.per + 1 + keys.ahead;
       kv_end = lim < 0 ? 0 : lim < Nk ? lim : Nk;
     } else if (CAUSAL) {
       const int lim = (qt + 1) * C::BM;
@@ -685,8 +691,8 @@ static __device__ __forceinline__ void bwd_dq(
       lse2 *= 1.4426950408889634f;
       if (Keys::PREFIX && lse2 == -INFINITY) lse2 = INFINITY;  // a row without keys: P = exp2(s - inf) = 0
       if (g == 0 && qrow < q_end) {
-        Dws[(size_t)head * Nq + qrow] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
-        LSE2ws[(size_t)head * Nq + qrow] = lse2;
+        Dws[stat] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
+        LSE2ws[stat] = lse2;
       }
     }
 #pragma unroll
@@ -704,7 +710,8 @@ static __device__ __forceinline__ void bwd_dq(
 
     // last key this lane's query attends to, less the 4 g that every register's key contains: the mask is one
     // compare with a constant per element
-    const int last_key = (Keys::PREFIX ? (qrow < Nk - keys.ahead ? qrow + keys.ahead : Nk - 1)
+    const int query = Keys::PREFIX ? qrow / keys.per : qrow;
+    const int last_key = (Keys::PREFIX ? (query < Nk - keys.ahead ? query + keys.ahead : Nk - 1)
                                        : (CAUSAL && qrow < Nk ? qrow : Nk - 1)) - 4 * g;
     // One iteration, compiled twice: MASKED for tiles that the diagonal or the end of the keys
     // crosses, and without any mask arithmetic for all the others.
@@ -716,7 +723,7 @@ static __device__ __forceinline__ void bwd_dq(
       const bool of_prefix = Keys::PREFIX && (j < np || j >= np_part);
       const int k0 = (!Keys::PREFIX ? j : of_prefix ? (j < np ? j : np) : j - np) * C::BN;
       // wave-uniform: skip tiles entirely above the diagonal (they are among the masked ones)
-      if (!MASKED || !CAUSAL || of_prefix || k0 <= q0 + 31 + keys.ahead) {
+      if (!MASKED || !CAUSAL || of_prefix || k0 <= (Keys::PREFIX ? (q0 + 31) / keys.per + keys.ahead : q0 + 31)) {
         SPARK_LDS const char* kb = smem;  // + off.* (which carry the buffer bit)
         SPARK_LDS const char* vb = smem + C::TILE;
 
@@ -858,7 +865,7 @@ static __device__ __forceinline__ void bwd_dq(
     // iterations, and with it the number of barriers, does not.
     int n_plain = Nk / C::BN;
     if constexpr (Keys::PREFIX) {
-      const int first = q0 + keys.ahead + 1;  // suffix keys that the wave's first row sees
+      const int first = q0 / keys.per + keys.ahead + 1;  // suffix keys that the wave's first row sees
       if (first / C::BN < n_plain) n_plain = first < 0 ? 0 : first / C::BN;
       n_plain += np;
       if (n_plain > np_part) n_plain = np_part;
@@ -869,11 +876,17 @@ static __device__ __forceinline__ void bwd_dq(
     int j = 0;
     for (; j < n_plain; ++j) iteration(j, std::false_type{});
     for (; j < nt; ++j) iteration(j, std::true_type{});
-    if constexpr (Keys::PREFIX) {  // rows not in use: zeros
+    if constexpr (Keys::PREFIX) {
+      SPARK_LDS char* ob = smem + wave * 32 * C::OSTR;
+      const float mul = qrow < q_end ? scale : 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dq[dt][r] = qrow < q_end ? dq[dt][r] : 0.f;
+        for (int r = 0; r < 16; ++r) dq[dt][r] = qrow < q_end ? dq[dt][r] : 0.f;  // rows not in use: zeros
+      store_transposed_to<T, D, C::OSTR>(dq, mul, ob, lane, [&](int row) -> T* {
+        return q0 + row < Nq ? dQ + keys.offset(mdq, q0 + row) : nullptr;
+      }, dh);
+      return;
     }
 
     SPARK_LDS char* ob = smem + wave * 32 * C::OSTR;

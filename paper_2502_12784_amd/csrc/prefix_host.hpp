@@ -28,6 +28,8 @@ int make_prefix(PrefixProblem* p, int G, int B, int H, int Hkv, int Nq, int P, i
   if (!isfinite(scale) || !(scale > 0.f)) return SPARK_ERR_SHAPE;
   const int64_t n = Nq > P ? (Nq > S ? Nq : S) : (P > S ? P : S);
   if ((n + 256) * d * 2 >= (int64_t)1 << 31) return SPARK_ERR_SHAPE;
+  // packed rows of a sequence (query, head) are counted in 31 bits, and so are a tile's worth more
+  if ((int64_t)Nq * (H / Hkv) >= (int64_t)1 << 30) return SPARK_ERR_SHAPE;
   if ((int64_t)B * H >= (int64_t)1 << 24 || (int64_t)B * H * ((n + 31) / 32) >= (int64_t)1 << 31) return SPARK_ERR_SHAPE;
   p->G = G; p->B = B; p->H = H; p->Hkv = Hkv; p->Nq = Nq; p->P = P; p->S = S; p->dh = d; p->causal = causal != 0;
   return SPARK_OK;
@@ -40,15 +42,22 @@ int launch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, float scale, 
   static std::atomic<uint64_t> ready{0};
   const int attr = ensure_smem(kernel, C::SMEM, ready);
   if (attr != SPARK_OK) return attr;
-  const int nqt = (p.Nq + C::BM - 1) / C::BM;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.H * nqt)), dim3(64 * NW), C::SMEM, st, p, static_cast<T*>(O), LSE, nqt,
+  const int nqt = (p.Nq * (p.H / p.Hkv) + C::BM - 1) / C::BM;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(64 * NW), C::SMEM, st, p, static_cast<T*>(O), LSE, nqt,
                      scale * 1.4426950408889634f);
   return launch_ok("forward kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
+// Workgroups of 8 waves (256 rows, one per CU) instead of 4: the rule of wide_workgroups in spark_mha.hip, for the same loop.
+bool prefix_wide(const PrefixProblem& p) {
+  const int64_t rows = (int64_t)p.Nq * (p.H / p.Hkv), owners = (int64_t)p.B * p.Hkv;
+  const int64_t wide = owners * ((rows + 255) / 256), narrow = owners * ((rows + 127) / 128);
+  return (int64_t)p.P + p.S >= 2048 && (wide >= 512 || narrow >= 896 || (wide <= 256 && narrow > 256));
+}
+
 // Whether the rows are packed and the keys go to several workgroups in runs (prefix_parts.hpp).
 bool prefix_packed(const PrefixProblem& p) {
-  return p.Nq <= 32 || (int64_t)p.B * p.H * ((p.Nq + 127) / 128) < 256;
+  return p.Nq <= 32 || (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128) < 256;
 }
 PrefixParts prefix_runs(const PrefixProblem& p) {
   PrefixParts s{};
@@ -88,8 +97,16 @@ int launch_prefix_parts(const PrefixProblem& p, void* O, float* LSE, void* works
   const int grid = s.p_items + p.B * p.Hkv * s.s_tiles * s.s_parts;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), SMEM, st, p, s, scale * 1.4426950408889634f);
   if (!launch_ok("forward kernel (prefix, in runs)")) return SPARK_ERR_LAUNCH;
-  hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W>), dim3((unsigned)(p.B * p.H * p.Nq)), dim3(256), 0, st, p, s.partial,
-                     s.p_parts + s.s_parts, static_cast<T*>(O), LSE);
+  // up to four parts are requested by one lane together: more lanes to a row only for more
+  const int parts = s.p_parts + s.s_parts;
+  const int64_t rows = (int64_t)p.B * p.H * p.Nq;
+  constexpr int SIDE = 256 / (W / 4);
+  if (parts <= 4)
+    hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W, 1>), dim3((unsigned)((rows + SIDE - 1) / SIDE)), dim3(256), 0, st, p,
+                       s.partial, parts, static_cast<T*>(O), LSE);
+  else
+    hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W, SIDE>), dim3((unsigned)rows), dim3(256), 0, st, p, s.partial, parts,
+                       static_cast<T*>(O), LSE);
   return launch_ok("forward merge kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
@@ -101,8 +118,9 @@ int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, void* works
     return launch_prefix_parts<T, 128>(p, O, LSE, workspace, scale, st);
   }
   if (p.dh <= 64) return launch_prefix_fwd<T, 64, 4, false>(p, O, LSE, scale, st);
-  if (p.dh <= 96) return launch_prefix_fwd<T, 96, 4, false>(p, O, LSE, scale, st);
-  return launch_prefix_fwd<T, 128, 4, false>(p, O, LSE, scale, st);
+  const bool wide = prefix_wide(p);
+  if (p.dh <= 96) return wide ? launch_prefix_fwd<T, 96, 8, true>(p, O, LSE, scale, st) : launch_prefix_fwd<T, 96, 4, false>(p, O, LSE, scale, st);
+  return wide ? launch_prefix_fwd<T, 128, 8, true>(p, O, LSE, scale, st) : launch_prefix_fwd<T, 128, 4, false>(p, O, LSE, scale, st);
 }
 
 // Workgroups that share the rows of a prefix tile: enough that such a tile takes no longer than its share of the chip's
@@ -134,8 +152,8 @@ int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, 
     static std::atomic<uint64_t> ready{0};
     const int attr = ensure_smem(kernel, C::SMEM, ready);
     if (attr != SPARK_OK) return attr;
-    const int nqt = (p.Nq + C::BM - 1) / C::BM;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.H * nqt)), dim3(256), C::SMEM, st, p, static_cast<const T*>(O), gr, nqt,
+    const int nqt = (p.Nq * (p.H / p.Hkv) + C::BM - 1) / C::BM;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(256), C::SMEM, st, p, static_cast<const T*>(O), gr, nqt,
                        scale);
     if (!launch_ok("dQ kernel (prefix)")) return SPARK_ERR_LAUNCH;
   }

@@ -32,23 +32,21 @@ static __device__ __forceinline__ int length_of(const int* lens, int i, int most
 // A query ahead that hides no suffix key: less than 2^31 with any row index (below 2^27) added.
 constexpr int ALL_AHEAD = 1 << 30;
 
-// What one (sequence, head) attends to.  `flat` orders them by prefix and head of keys, so that those that share keys are
-// neighbours and run on the same XCD.
+// What the query heads of one (sequence, head of keys) attend to.  `flat` orders them by prefix and head of keys, so that
+// those that share keys are neighbours and run on the same XCD.
 struct PrefixHead {
-  int b, h, hk, grp;
-  int P, rows, S, ahead;
+  int b, hk, grp;
+  int P, q, S, ahead;  // lengths
   __device__ __forceinline__ PrefixHead(const PrefixProblem& p, int flat) {
-    const int per = p.H / p.Hkv, seqs = p.B / p.G;
-    const int sub = flat % (seqs * per);
-    flat /= seqs * per;
+    const int seqs = p.B / p.G, sub = flat % seqs;
+    flat /= seqs;
     hk = flat % p.Hkv;
     grp = flat / p.Hkv;
-    b = grp * seqs + sub / per;
-    h = hk * per + sub % per;
+    b = grp * seqs + sub;
     P = length_of(p.prefix_lens, grp, p.P);
-    rows = length_of(p.q_lens, b, p.Nq);
+    q = length_of(p.q_lens, b, p.Nq);
     S = length_of(p.s_lens, b, p.S);
-    ahead = p.causal ? S - rows : ALL_AHEAD;
+    ahead = p.causal ? S - q : ALL_AHEAD;
   }
 };
 template <typename T>
@@ -59,7 +57,17 @@ static __device__ __forceinline__ uint32_t span_or_none(const TensorMap& m, int 
   return n ? head_span_bytes(m, n, dh) : 0;
 }
 
-// Rows [row0, row1) of one head of an output, all zeros, by the whole workgroup.
+// Packed rows [row0, row1) of an output (`out`: of the first of their heads), all zeros, by the whole workgroup; and rows
+// of one head.
+template <typename T>
+static __device__ __forceinline__ void zero_rows(T* out, const TensorMap& m, const PrefixAndSuffix<T>& keys, int row0, int row1,
+                                                 int dh) {
+  const int chunks = dh / 8;
+  for (int i = threadIdx.x; i < (row1 - row0) * chunks; i += blockDim.x) {
+    const int r = i / chunks;
+    *reinterpret_cast<u32x4*>(out + keys.offset(m, row0 + r) + (i - r * chunks) * 8) = u32x4{0, 0, 0, 0};
+  }
+}
 template <typename T>
 static __device__ __forceinline__ void zero_rows(T* head, const TensorMap& m, int row0, int row1, int dh) {
   const int chunks = dh / 8;
@@ -69,24 +77,13 @@ static __device__ __forceinline__ void zero_rows(T* head, const TensorMap& m, in
   }
 }
 
-template <typename T, int D, int NW, bool PAIR>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_prefix_fwd_kernel(
-    PrefixProblem p, T* __restrict__ O, float* __restrict__ LSE, int nqt, float scale_log2) {
-  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
-  const int flat = logical / nqt, item = logical - flat * nqt;
-  const PrefixHead x(p, flat);
-  const int head = x.b * p.H + x.h;
-  constexpr int BM = FwdCfg<D, NW, PAIR>::BM;
-  // the causal loop takes the tiles from the last (longest) one on
-  const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < p.Nq ? row0 + BM : p.Nq;
-  if (row0 >= x.rows || (x.P == 0 && (x.S == 0 || row1 + x.ahead <= 0))) {  // no row in use, or no key for any
-    zero_rows(O + (size_t)x.b * (size_t)p.mo.batch + (size_t)x.h * (size_t)p.mo.head, p.mo, row0, row1, p.dh);
-    for (int i = row0 + threadIdx.x; i < row1; i += 64 * NW) LSE[(size_t)head * p.Nq + i] = -INFINITY;
-    return;
-  }
+// The keys of the workgroup's tile of packed rows.
+template <typename T>
+static __device__ __forceinline__ PrefixAndSuffix<T> keys_of(const PrefixProblem& p, const PrefixHead& x, int item) {
   PrefixAndSuffix<T> keys;
-  keys.head = head;
   keys.item = item;
+  keys.per = p.H / p.Hkv;
+  keys.queries = p.Nq;
   keys.Kp = head_of<T>(p.Kp, p.mkp, x.grp, x.hk);
   keys.Vp = head_of<T>(p.Vp, p.mvp, x.grp, x.hk);
   keys.kp_row_bytes = (uint32_t)p.mkp.row * 2;
@@ -94,11 +91,32 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_
   keys.kp_bytes = span_or_none(p.mkp, x.P, p.dh);
   keys.vp_bytes = span_or_none(p.mvp, x.P, p.dh);
   keys.P = x.P;
-  keys.rows = x.rows;
+  keys.rows = x.q * keys.per;
   keys.ahead = x.ahead;
-  fwd_tiles<T, D, true, false, NW, PAIR>(static_cast<const T*>(p.Q), head_of<T>(p.Ks, p.mks, x.b, x.hk),
-                                         head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, LSE, p.mq, p.mks, p.mvs, p.mo, p.H, p.Nq,
-                                         x.S, p.dh, nqt, 0, scale_log2, Dropout{}, keys);
+  return keys;
+}
+
+template <typename T, int D, int NW, bool PAIR>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? (D == 64 ? 3 : 2) : 1) void mha_prefix_fwd_kernel(
+    PrefixProblem p, T* __restrict__ O, float* __restrict__ LSE, int nqt, float scale_log2) {
+  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int flat = logical / nqt, item = logical - flat * nqt;
+  const PrefixHead x(p, flat);
+  const PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
+  const int h0 = x.hk * keys.per, all = p.Nq * keys.per;
+  O += (size_t)x.b * (size_t)p.mo.batch + (size_t)h0 * (size_t)p.mo.head;
+  LSE += ((size_t)x.b * p.H + h0) * (size_t)p.Nq;
+  constexpr int BM = FwdCfg<D, NW, PAIR>::BM;
+  // the causal loop takes the tiles from the last (longest) one on
+  const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < all ? row0 + BM : all;
+  if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
+    zero_rows(O, p.mo, keys, row0, row1, p.dh);
+    for (int r = row0 + threadIdx.x; r < row1; r += 64 * NW) LSE[keys.stat(r)] = -INFINITY;
+    return;
+  }
+  fwd_tiles<T, D, true, false, NW, PAIR>(head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk),
+                                         head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, LSE, p.mq, p.mks, p.mvs, p.mo, p.H, all, x.S,
+                                         p.dh, nqt, 0, scale_log2, Dropout{}, keys);
 }
 
 template <typename T> struct PrefixGrads {
@@ -117,33 +135,25 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_dq_kernel(PrefixProblem p, 
   const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
   const int flat = logical / nqt, item = logical - flat * nqt;
   const PrefixHead x(p, flat);
-  const int head = x.b * p.H + x.h;
+  const PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
+  const int h0 = x.hk * keys.per, all = p.Nq * keys.per;
+  T* const dQ = gr.dQ + (size_t)x.b * (size_t)gr.mdq.batch + (size_t)h0 * (size_t)gr.mdq.head;
+  const size_t stats = ((size_t)x.b * p.H + h0) * (size_t)p.Nq;
   constexpr int BM = BwdQCfg<D, true, false>::BM;
-  const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < p.Nq ? row0 + BM : p.Nq;
-  if (row0 >= x.rows || (x.P == 0 && (x.S == 0 || row1 + x.ahead <= 0))) {  // no row in use, or no key for any
-    zero_rows(gr.dQ + (size_t)x.b * (size_t)gr.mdq.batch + (size_t)x.h * (size_t)gr.mdq.head, gr.mdq, row0, row1, p.dh);
-    for (int i = row0 + threadIdx.x; i < row1; i += 256) {
-      gr.Dws[(size_t)head * p.Nq + i] = 0.f;
-      gr.LSE2ws[(size_t)head * p.Nq + i] = INFINITY;
+  const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < all ? row0 + BM : all;
+  if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
+    zero_rows(dQ, gr.mdq, keys, row0, row1, p.dh);
+    for (int r = row0 + threadIdx.x; r < row1; r += 256) {
+      gr.Dws[stats + keys.stat(r)] = 0.f;
+      gr.LSE2ws[stats + keys.stat(r)] = INFINITY;
     }
     return;
   }
-  PrefixAndSuffix<T> keys;
-  keys.head = head;
-  keys.item = item;
-  keys.Kp = head_of<T>(p.Kp, p.mkp, x.grp, x.hk);
-  keys.Vp = head_of<T>(p.Vp, p.mvp, x.grp, x.hk);
-  keys.kp_row_bytes = (uint32_t)p.mkp.row * 2;
-  keys.vp_row_bytes = (uint32_t)p.mvp.row * 2;
-  keys.kp_bytes = span_or_none(p.mkp, x.P, p.dh);
-  keys.vp_bytes = span_or_none(p.mvp, x.P, p.dh);
-  keys.P = x.P;
-  keys.rows = x.rows;
-  keys.ahead = x.ahead;
-  bwd_dq<T, D, true, false, false, IN_ORDER>(static_cast<const T*>(p.Q), head_of<T>(p.Ks, p.mks, x.b, x.hk),
-                                             head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, gr.dO, gr.LSE, gr.Dws, gr.LSE2ws, gr.dQ,
-                                             p.mq, p.mks, p.mvs, p.mo, gr.mdo, gr.mdq, p.H, p.Nq, x.S, p.dh, nqt, 0, scale,
-                                             scale * 1.4426950408889634f, Dropout{}, head, item, keys);
+  bwd_dq<T, D, true, false, false, IN_ORDER>(
+      head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk), head_of<T>(p.Vs, p.mvs, x.b, x.hk),
+      head_of<T>(O, p.mo, x.b, h0), head_of<T>(gr.dO, gr.mdo, x.b, h0), gr.LSE + stats, gr.Dws + stats, gr.LSE2ws + stats, dQ,
+      p.mq, p.mks, p.mvs, p.mo, gr.mdo, gr.mdq, p.H, all, x.S, p.dh, nqt, 0, scale, scale * 1.4426950408889634f, Dropout{}, 0,
+      item, keys);
 }
 
 // The query rows that see a key tile, in stages of 64 of one (sequence, head), for bwd_dkdv_pipe; and where its sums go.
@@ -161,7 +171,9 @@ template <typename T, int D> struct GroupRows {
   const int* q_lens;
   TensorMap mq, mdo;
   int H, Nq, dh;
-  int b, h, h0, h1, left;  // present pair, the heads of the tile, pairs left with it
+  int b, h;                // present pair
+  int h0, h1, b_end;       // the heads that share the tile, the end of its sequences
+  int left;                // stages left behind the present one, at most
   int k0;                  // causal: the tile's first key, with S keys in the suffix; -1: every row sees the tile
   int S;
   int blocks, ahead;       // of the present pair
@@ -192,24 +204,62 @@ template <typename T, int D> struct GroupRows {
     return true;
   }
   __device__ __forceinline__ bool next_pair() {
-    while (left > 0) {
-      --left;
+    for (;;) {
       if (++h == h1) {
         h = h0;
-        ++b;
+        if (++b == b_end) return false;
       }
       if (enter()) return true;
     }
-    return false;
   }
   // The first stage; false if no row sees the tile.
-  __device__ __forceinline__ bool start() { return enter() || next_pair(); }
+  __device__ __forceinline__ bool start() { return left >= 0 && (enter() || next_pair()); }
   __device__ __forceinline__ bool advance() {
+    if (--left < 0) return false;
     if (s.block + 1 < blocks) {
       ++s.block;
       return true;
     }
     return next_pair();
+  }
+  // Start at stage `skip` of a prefix tile's, counted over its pairs in order, and take `count` of them.  The wave's lanes add
+  // up the sequences' blocks, 64 sequences at a time.
+  __device__ __forceinline__ bool start_at(int skip, int count) {
+    const int per = h1 - h0, lane = threadIdx.x & 63;
+    left = count - 1;
+    if (count <= 0) return false;
+    for (; b < b_end; b += 64) {
+      int own = 0;  // stages of the lane's sequence
+      if (b + lane < b_end) own = (length_of(q_lens, b + lane, Nq) + 63) / 64 * per;
+      int sum = own;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const int other = __shfl_up(sum, m);
+        if (lane >= m) sum += other;
+      }
+      const uint64_t behind = __ballot(sum > skip);  // the first such sequence holds the stage
+      if (behind) {
+        const int at = __builtin_ctzll(behind);
+        b += at;
+        skip -= __builtin_amdgcn_readlane(sum - own, at);
+        const int each = __builtin_amdgcn_readlane(own, at) / per;
+        h = h0 + skip / each;
+        if (!enter()) return false;
+        s.block += skip % each;
+        return true;
+      }
+      skip -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+  }
+  // All stages of sequences [b, b_end).
+  __device__ __forceinline__ int stages() const {
+    const int per = h1 - h0, lane = threadIdx.x & 63;
+    int own = 0;
+    for (int x = b + lane; x < b_end; x += 64) own += (length_of(q_lens, x, Nq) + 63) / 64 * per;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) own += __shfl_xor(own, m);
+    return __builtin_amdgcn_readfirstlane(own);
   }
   __device__ __forceinline__ void store(const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32], SPARK_LDS char* ob, int k0w,
                                         int lane, float scale) const {
@@ -259,6 +309,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
   rows.dh = p.dh;
   rows.partial = nullptr;
   int hk, tile;
+  bool any = false;  // whether a row sees the tile
   const T *K, *V;
   TensorMap mk, mv;
   if (of_prefix) {
@@ -266,13 +317,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     tile = logical % p_tiles;
     const int unit = logical / p_tiles, part = unit % gr.parts, owner = unit / gr.parts, grp = owner / p.Hkv;
     hk = owner - grp * p.Hkv;
-    const int pairs = seqs * per, begin = (int)((int64_t)pairs * part / gr.parts),
-              end = (int)((int64_t)pairs * (part + 1) / gr.parts);
-    rows.b = grp * seqs + begin / per;
-    rows.h0 = hk * per;
-    rows.h = rows.h0 + begin % per;
-    rows.left = end - begin - 1;
+    rows.b = grp * seqs;
+    rows.b_end = rows.b + seqs;
+    rows.h = rows.h0 = hk * per;
+    rows.h1 = rows.h0 + per;
     rows.k0 = -1;
+    const int stages = rows.stages(), begin = (int)((int64_t)stages * part / gr.parts);
+    any = rows.start_at(begin, (int)((int64_t)stages * (part + 1) / gr.parts) - begin);
     rows.S = 0;
     rows.keys = length_of(p.prefix_lens, grp, p.P);
     rows.all = p.P;
@@ -286,13 +337,16 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     mk = p.mkp;
     mv = p.mvp;
   } else {
-    const int logical = xcd_contiguous(blockIdx.x - first, gridDim.x - first);
-    tile = logical % s_tiles;
-    const int owner = logical / s_tiles, b = owner / p.Hkv;
+    // the first tiles of all suffixes first: more rows see them
+    const int owners = p.B * p.Hkv, id = (int)blockIdx.x - first;
+    tile = id / owners;
+    const int owner = xcd_contiguous(id - tile * owners, owners), b = owner / p.Hkv;
     hk = owner - b * p.Hkv;
     rows.b = b;
+    rows.b_end = b + 1;
     rows.h = rows.h0 = hk * per;
-    rows.left = per - 1;
+    rows.h1 = rows.h0 + per;
+    rows.left = 1 << 30;
     rows.keys = rows.S = length_of(p.s_lens, b, p.S);
     rows.k0 = p.causal ? tile * BN : -1;
     rows.all = p.S;
@@ -305,9 +359,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     mk = p.mks;
     mv = p.mvs;
   }
-  rows.h1 = rows.h0 + per;
   const int k0 = tile * BN, k1 = k0 + BN < rows.all ? k0 + BN : rows.all;
-  const bool none = k0 >= rows.keys || !rows.start();
+  if (!of_prefix) any = k0 < rows.keys && rows.start();
+  const bool none = k0 >= rows.keys || !any;
   if (!rows.partial) {  // rows of keys that do not exist, or that no query sees
     const int from = none ? k0 : rows.keys > k0 ? rows.keys : k0;
     if (from < k1) {

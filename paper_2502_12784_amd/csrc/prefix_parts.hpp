@@ -8,7 +8,7 @@
 //     with many rows this is a matrix product; up to 32 rows in the split forward's loop, which is a read of K and V;
 //   * runs of a sequence's suffix against its own packed rows (heads, queries), 32 to a tile, four waves with a stream of
 //     keys each (fwd_split_tiles): a read of K and V;
-//   * mha_prefix_merge_kernel: a workgroup per row adds its partial results, all of them requested at once.
+//   * mha_prefix_merge_kernel adds a row's partial results, as many of them requested at once as there are lanes for.
 // Both kinds of runs are in one grid, two workgroups to a CU: the products of the prefix overlap with the reads of the
 // suffixes.  A partial result is lds_row<D> + 4 floats: O, unnormalised, m, l (0: the run had no key for the row).
 #pragma once
@@ -125,23 +125,23 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_parts_kernel(PrefixProblem 
                                                  scale_log2, Dropout{}, 1, nullptr, rows);
 }
 
-// One row's parts: W / 4 lanes each, 256 / (W / 4) of them side by side.
-template <typename T, int W>
+// A row's parts: W / 4 lanes to a part, SIDE of them side by side, four requested together by each; as many rows to a
+// workgroup as then fit.
+template <typename T, int W, int SIDE>
 __global__ __launch_bounds__(256) void mha_prefix_merge_kernel(PrefixProblem p, const float* __restrict__ partial, int parts,
                                                                T* __restrict__ O, float* __restrict__ LSE) {
   using v4 = typename Frag<T>::v4;
-  constexpr int LPR = W / 4, SIDE = 256 / LPR;
-  __shared__ float top[SIDE];
-  __shared__ f32x4 sums[SIDE][LPR + 1];
-  const size_t row = blockIdx.x;
+  constexpr int LPR = W / 4, ROWS = 256 / (LPR * SIDE);
+  __shared__ float top[ROWS][SIDE];
+  __shared__ f32x4 sums[ROWS][SIDE][LPR + 1];
+  const int c = threadIdx.x % LPR, side = threadIdx.x / LPR % SIDE, slot = threadIdx.x / (LPR * SIDE);
+  const size_t rows = (size_t)p.B * p.H * (size_t)p.Nq, row = (size_t)blockIdx.x * ROWS + slot;
   const int bh = (int)(row / (size_t)p.Nq), i = (int)(row - (size_t)bh * p.Nq), b = bh / p.H, h = bh - b * p.H;
-  const int side = threadIdx.x / LPR, c = threadIdx.x % LPR;
-  const bool used = i < length_of(p.q_lens, b, p.Nq);
+  const bool used = row < rows && i < length_of(p.q_lens, b, p.Nq);
   const float* x = partial + row * (size_t)parts * (W + 4);
   float m = -1e30f, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   if (used) {
-    // four parts at a time, so that their loads are in flight together
     for (int s0 = side; s0 < parts; s0 += 4 * SIDE) {
       f32x4 st[4], v[4];
 #pragma unroll
@@ -163,25 +163,29 @@ __global__ __launch_bounds__(256) void mha_prefix_merge_kernel(PrefixProblem p, 
       }
     }
   }
-  if (c == 0) top[side] = m;
-  __syncthreads();
-  float all = top[0];
+  if (SIDE > 1) {
+    if (c == 0) top[slot][side] = m;
+    __syncthreads();
+    float all = top[slot][0];
 #pragma unroll
-  for (int s = 1; s < SIDE; ++s) all = fmaxf(all, top[s]);
-  const float w = __builtin_amdgcn_exp2f(m - all);
+    for (int s = 1; s < SIDE; ++s) all = fmaxf(all, top[slot][s]);
+    const float w = __builtin_amdgcn_exp2f(m - all);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] *= w;
-  sums[side][c] = o;
-  if (c == 0) sums[side][LPR][0] = l * w;
-  __syncthreads();
-  if (side) return;
-  l = sums[0][LPR][0];
+    for (int e = 0; e < 4; ++e) o[e] *= w;
+    sums[slot][side][c] = o;
+    if (c == 0) sums[slot][side][LPR][0] = l * w;
+    m = all;
+    __syncthreads();
+    if (side) return;
+    l = sums[slot][0][LPR][0];
 #pragma unroll
-  for (int s = 1; s < SIDE; ++s) {
-    l += sums[s][LPR][0];
-    o += sums[s][c];
+    for (int s = 1; s < SIDE; ++s) {
+      l += sums[slot][s][LPR][0];
+      o += sums[slot][s][c];
+    }
   }
-  if (c == 0) LSE[row] = l == 0.f ? -INFINITY : (all + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  if (row >= rows) return;
+  if (c == 0) LSE[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   if (4 * c < p.dh) {
     const float inv = 1.0f / l;
     v4 pk;

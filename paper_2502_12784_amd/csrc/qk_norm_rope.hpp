@@ -296,23 +296,28 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormRope a) {
   }
 }
 
-// dw of one side from the partial sums, in their order: 32 columns to a workgroup.
+// dw of one side from the partial sums, in their order: 16 columns to a workgroup, 64 sums of every column side by side.
 __global__ __launch_bounds__(1024) void qk_norm_dw_kernel(const float* __restrict__ partial, float* __restrict__ dwq,
                                                           float* __restrict__ dwk, int d, int q_parts, int parts) {
-  __shared__ float sums[32][33];
-  const int c = threadIdx.x & 31, r = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  __shared__ float sums[64][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
   const int first = blockIdx.y == 0 ? 0 : q_parts, last = blockIdx.y == 0 ? q_parts : parts;
   float acc = 0.f;
   if (col < d) {
-#pragma unroll 8
-    for (int p = first + r; p < last; p += 32) acc += partial[(size_t)p * (size_t)d + col];
+    for (int p = first + r; p < last; p += 16 * 64) {  // sixteen requested together
+      float x[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) x[u] = p + u * 64 < last ? partial[(size_t)(p + u * 64) * (size_t)d + col] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 16; ++u) acc += x[u];
+    }
   }
   sums[r][c] = acc;
   __syncthreads();
   if (r == 0 && col < d) {
     acc = 0.f;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) acc += sums[i][c];
+    for (int i = 0; i < 64; ++i) acc += sums[i][c];
     (blockIdx.y == 0 ? dwq : dwk)[col] = acc;
   }
 }

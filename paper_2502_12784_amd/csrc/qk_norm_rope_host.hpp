@@ -135,7 +135,7 @@ int spark_qk_norm_rope_bwd(const void* Q, const void* K, const void* wq, const v
   rc = dtype == SPARK_F16 ? dispatch_qk<_Float16>(a, grid, true, interleaved != 0, st)
                           : dispatch_qk<__bf16>(a, grid, true, interleaved != 0, st);
   if (rc != SPARK_OK) return rc;
-  hipLaunchKernelGGL(qk_norm_dw_kernel, dim3((unsigned)((d + 31) / 32), 2), dim3(1024), 0, st, a.partial, dwq, dwk, d,
+  hipLaunchKernelGGL(qk_norm_dw_kernel, dim3((unsigned)((d + 15) / 16), 2), dim3(1024), 0, st, a.partial, dwq, dwk, d,
                      grid.x * a.q_groups, parts);
   return launch_ok("weight gradient kernel") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }

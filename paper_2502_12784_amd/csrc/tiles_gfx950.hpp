@@ -284,4 +284,31 @@ static __device__ __forceinline__ void store_transposed(const f32x16 (&acc)[D / 
   }
 }
 
+// The same to rows that lie anywhere: place(row) is where row 0 ... 31 goes, or nullptr.
+template <typename T, int D, int OSTR, typename Place>
+static __device__ __forceinline__ void store_transposed_to(const f32x16 (&acc)[D / 32], float mul, SPARK_LDS char* ob, int lane,
+                                                           Place place, int dh) {
+  using v4 = typename Frag<T>::v4;
+  constexpr int CPR = lds_row<D> / 8;
+  constexpr int RPP = 64 / CPR;
+  asm volatile("" : "+v"(lane));
+  const int g = lane >> 5, c32 = lane & 31;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      v4 pk;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) pk[e] = (T)(acc[dt][r4 * 4 + e] * mul);
+      lds_write(ob, c32 * OSTR + (dt * 32 + 8 * r4 + 4 * g) * 2, pk);
+    }
+#pragma unroll
+  for (int p = 0; p < 32 / RPP; ++p) {
+    const int row = p * RPP + lane / CPR, cc = lane % CPR;
+    const u32x4 v = lds_read16<u32x4>(ob, row * OSTR + cc * 16);
+    T* const out = place(row);
+    if (out && cc * 8 < dh) *reinterpret_cast<u32x4*>(out + cc * 8) = v;
+  }
+}
+
 }  // namespace spark
