@@ -59,23 +59,30 @@ bool prefix_wide(const PrefixProblem& p) {
 bool prefix_packed(const PrefixProblem& p) {
   return p.Nq <= 32 || (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128) < 256;
 }
+// The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
+// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4; 256 rows, 16384 keys, d = 128 in
+// two of 128: 50, two and a half times that in tiles of 32).  Its runs fill half of the chip's places; a prefix that is only
+// read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256
+// workgroups 23.1 / 23.0 / 23.8 / 25.6 / 25.9; 96 suffixes, 4001 keys 23.4 / 23.8 / 23.5 / 16.7 / 16.1; 256 rows, 16384 keys,
+// 128 / 256 / 384 / 512 58 / 51 / 55 / 63).
 PrefixParts prefix_runs(const PrefixProblem& p) {
   PrefixParts s{};
   const int64_t per = p.H / p.Hkv, rows = (int64_t)(p.B / p.G) * p.Nq * per;
   const int bn = p.dh <= 64 ? 64 : 32;
-  s.wide = rows > 32;
+  s.wide = rows > 96;
   s.p_tiles = p.P ? (int)((rows + (s.wide ? 127 : 31)) / (s.wide ? 128 : 32)) : 0;
   s.s_tiles = p.S ? (int)((p.Nq * per + 31) / 32) : 0;
   const int64_t n1 = (int64_t)p.G * p.Hkv * s.p_tiles, n2 = (int64_t)p.B * p.Hkv * s.s_tiles;
-  auto runs = [](int64_t units, int64_t items, int64_t most) {
-    int64_t n = items ? 256 / items : 0;
+  auto runs = [](int64_t places, int64_t items, int64_t units, int64_t most) {
+    int64_t n = items ? places / items : 0;
     if (n > units) n = units;
     if (n > most) n = most;
     return (int)(n < 1 ? 1 : n);
   };
+  const int64_t places = s.wide || n2 <= 256 ? 256 : n2 >= 416 ? 96 : 512 - n2;
   // at least four tiles of the wide loop to a run, or two rounds of the four key streams
-  s.p_parts = p.P ? runs(s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn), n1, 64) : 0;
-  s.s_parts = p.S ? runs((p.S + 8 * bn - 1) / (8 * bn), n2, 16) : 0;
+  s.p_parts = p.P ? runs(places, n1, s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn), 64) : 0;
+  s.s_parts = p.S ? runs(256, n2, (p.S + 8 * bn - 1) / (8 * bn), 16) : 0;
   s.p_items = (int)(n1 * s.p_parts);
   return s;
 }
@@ -97,16 +104,17 @@ int launch_prefix_parts(const PrefixProblem& p, void* O, float* LSE, void* works
   const int grid = s.p_items + p.B * p.Hkv * s.s_tiles * s.s_parts;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), SMEM, st, p, s, scale * 1.4426950408889634f);
   if (!launch_ok("forward kernel (prefix, in runs)")) return SPARK_ERR_LAUNCH;
-  // up to four parts are requested by one lane together: more lanes to a row only for more
+  // four parts are requested by a lane together: as many lanes side by side to a row as that leaves
   const int parts = s.p_parts + s.s_parts;
   const int64_t rows = (int64_t)p.B * p.H * p.Nq;
-  constexpr int SIDE = 256 / (W / 4);
-  if (parts <= 4)
-    hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W, 1>), dim3((unsigned)((rows + SIDE - 1) / SIDE)), dim3(256), 0, st, p,
-                       s.partial, parts, static_cast<T*>(O), LSE);
-  else
-    hipLaunchKernelGGL((mha_prefix_merge_kernel<T, W, SIDE>), dim3((unsigned)rows), dim3(256), 0, st, p, s.partial, parts,
-                       static_cast<T*>(O), LSE);
+  constexpr int MOST = 256 / (W / 4);
+  auto merge = parts <= 4    ? mha_prefix_merge_kernel<T, W, 1>
+               : parts <= 8  ? mha_prefix_merge_kernel<T, W, 2>
+               : parts <= 16 ? mha_prefix_merge_kernel<T, W, 4>
+                             : mha_prefix_merge_kernel<T, W, MOST>;
+  const int side = parts <= 4 ? 1 : parts <= 8 ? 2 : parts <= 16 ? 4 : MOST, each = MOST / side;
+  hipLaunchKernelGGL(merge, dim3((unsigned)((rows + each - 1) / each)), dim3(256), 0, st, p, s.partial, parts,
+                     static_cast<T*>(O), LSE);
   return launch_ok("forward merge kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
@@ -123,25 +131,50 @@ int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, void* works
   return wide ? launch_prefix_fwd<T, 128, 8, true>(p, O, LSE, scale, st) : launch_prefix_fwd<T, 128, 4, false>(p, O, LSE, scale, st);
 }
 
-// Workgroups that share the rows of a prefix tile: enough that such a tile takes no longer than its share of the chip's
-// work, all of a workgroup's stages counted alike (a suffix tile's rows, if causal, as half).
-int prefix_parts(const PrefixProblem& p) {
-  if (p.P == 0) return 1;
-  const int64_t slots = 256 * (p.dh <= 64 ? 2 : 1), pairs = (int64_t)(p.B / p.G) * (p.H / p.Hkv), blocks = (p.Nq + 63) / 64;
+// How many workgroups share the rows of a key tile in the dK/dV kernel, by an estimate of its time.  Counted in stages (64 rows
+// of a head against 128 keys, some 2 us): a workgroup costs three more, the parts of dKp and dVp are written and read once,
+// and the end of the grid waits for half a short item.  A suffix tile is cut into runs of half a prefix tile's stages, at least
+// four.  (us, step of 6 sequences x 6 heads over 2 x 333 behind 700, d = 80, 1 / 3 / 5 / 6 parts with whole suffix tiles - / 77 / 89 / 90;
+// 16 sequences x 16 over 4 x 512 behind 1024, 2 / 3 / 4 / 6 parts 399 / 386 / 392 / 385.)
+struct PrefixShares {
+  int parts, s_parts, s_run;
+};
+PrefixShares prefix_shares(const PrefixProblem& p) {
+  const double slots = 256 * (p.dh <= 64 ? 2 : 1), columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
+  const int64_t per = p.H / p.Hkv, blocks = (p.Nq + 63) / 64;
   const int64_t n1 = (int64_t)p.G * p.Hkv * ((p.P + 127) / 128), n2 = (int64_t)p.B * p.Hkv * ((p.S + 127) / 128);
-  const int64_t w1 = pairs * blocks, w2 = (p.H / p.Hkv) * blocks;
-  const int64_t share = (n1 * w1 + n2 * w2 / (p.causal ? 2 : 1)) / slots + 1;
-  int64_t parts = (w1 + share - 1) / share;
-  if (parts > 32) parts = 32;
-  if (parts > pairs) parts = pairs;
-  if (n1 * parts >= (int64_t)1 << 30) parts = 1;
-  return parts < 1 ? 1 : (int)parts;
+  const int64_t w1 = p.B / p.G * per * blocks, w2 = per * blocks;
+  auto run_of = [&](int64_t parts) {
+    int64_t run = p.P ? w1 / parts / 2 : (n2 * w2 + 511) / 512;
+    if (run < 4) run = 4;
+    if (run < (w2 + 15) / 16) run = (w2 + 15) / 16;  // sixteen runs at most
+    return run < w2 ? run : w2;
+  };
+  int64_t best = 1;
+  double least = 0;
+  for (int64_t parts = 1; parts <= 32 && parts <= w1 && p.P; ++parts) {
+    const double run = (double)run_of(parts), item = (double)w1 / parts + 3, runs = (double)((w2 + (int64_t)run - 1) / (int64_t)run);
+    const double s_item = run + 3, s_work = (p.causal ? 0.5 : 1.0) * w2 + 3 * runs;
+    const double work = (n1 * parts * item + n2 * s_work) / slots, longest = item > s_item ? item : s_item;
+    double time = work + (item < s_item ? item : s_item) / 2;
+    if (n1 * parts + n2 * runs <= slots || time < longest) time = longest;
+    if (parts > 1) time += parts * n1 * 128.0 * columns * 16 / 8e6;
+    if (parts == 1 || time < least) {
+      best = parts;
+      least = time;
+    }
+  }
+  if (n1 * best >= (int64_t)1 << 30) best = 1;
+  int64_t run = run_of(best);
+  if (n2 * ((w2 + run - 1) / run) >= (int64_t)1 << 30) run = w2;
+  return PrefixShares{(int)best, p.S ? (int)((w2 + run - 1) / run) : 1, (int)run};
 }
 size_t prefix_stats_bytes(const PrefixProblem& p) { return ((size_t)p.B * p.H * p.Nq * 8 + 255) & ~(size_t)255; }
 size_t prefix_bwd_workspace(const PrefixProblem& p) {
-  const int parts = prefix_parts(p);
+  const PrefixShares x = prefix_shares(p);
   const size_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
-  return prefix_stats_bytes(p) + (parts > 1 ? (size_t)parts * p.G * p.Hkv * p.P * columns * 8 : 0);
+  return prefix_stats_bytes(p) + (x.parts > 1 ? (size_t)x.parts * p.G * p.Hkv * p.P * columns * 8 : 0) +
+         (x.s_parts > 1 ? (size_t)x.s_parts * p.B * p.Hkv * p.S * columns * 8 : 0);
 }
 
 template <typename T, int D>
@@ -163,14 +196,16 @@ int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, 
   const int attr = ensure_smem(kernel, C::SMEM, ready);
   if (attr != SPARK_OK) return attr;
   const int p_tiles = (p.P + C::BN - 1) / C::BN, s_tiles = (p.S + C::BN - 1) / C::BN;
-  const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles;
+  const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles * gr.s_parts;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), C::SMEM, st, p, gr, p_tiles, s_tiles, first, scale);
   if (!launch_ok("dK/dV kernel (prefix)")) return SPARK_ERR_LAUNCH;
-  if (gr.parts == 1) return SPARK_OK;
+  if (gr.parts == 1 && gr.s_parts == 1) return SPARK_OK;
   constexpr int RPB = 256 * 4 / D;
-  const int64_t rows = (int64_t)p.G * p.Hkv * p.P;
-  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, st, p, gr, scale);
-  return launch_ok("sum of the prefix's parts") ? SPARK_OK : SPARK_ERR_LAUNCH;
+  const int64_t p_rows = gr.parts > 1 ? (int64_t)p.G * p.Hkv * p.P : 0, s_rows = gr.s_parts > 1 ? (int64_t)p.B * p.Hkv * p.S : 0;
+  const int p_blocks = (int)((p_rows + RPB - 1) / RPB), s_blocks = (int)((s_rows + RPB - 1) / RPB);
+  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)(p_blocks + s_blocks)), dim3(256), 0, st, p, gr, p_blocks,
+                     scale);
+  return launch_ok("sum of the parts (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
 struct PrefixGradArgs {
@@ -195,7 +230,12 @@ int dispatch_prefix_bwd(const PrefixProblem& p, const void* O, const PrefixGradA
   gr.Dws = static_cast<float*>(a.workspace);
   gr.LSE2ws = gr.Dws + (size_t)p.B * p.H * p.Nq;
   gr.partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + prefix_stats_bytes(p));
-  gr.parts = prefix_parts(p);
+  const PrefixShares x = prefix_shares(p);
+  gr.parts = x.parts;
+  gr.s_parts = x.s_parts;
+  gr.s_run = x.s_run;
+  const int64_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
+  gr.partial_s = gr.partial + (x.parts > 1 ? (size_t)x.parts * p.G * p.Hkv * p.P * columns * 2 : 0);
   if (p.dh <= 64) return launch_prefix_bwd<T, 64>(p, O, gr, scale, st);
   if (p.dh <= 96) return launch_prefix_bwd<T, 96>(p, O, gr, scale, st);
   return launch_prefix_bwd<T, 128>(p, O, gr, scale, st);

@@ -8,7 +8,8 @@
 // part.  dQ walks both parts as the forward does.  dK and dV of a suffix tile sum over the rows of the heads that share it,
 // those of a prefix tile over the rows of all sequences of the group too: the loop of bwd_dkdv_pipe, whose stages of 64 rows
 // then come from one (sequence, head) after the other.  That sum is long and there are few such tiles: `parts` workgroups
-// share it, each leaves its part in fp32, and a small kernel adds them in their order.
+// share it, and likewise a suffix tile's where the batch is small; each leaves its part in fp32, and a small kernel adds them
+// in their order.
 #pragma once
 #include "bwd_kernels.hpp"
 #include "fwd_kernel.hpp"
@@ -126,7 +127,20 @@ template <typename T> struct PrefixGrads {
   const float* LSE;
   float *Dws, *LSE2ws;  // [B,H,Nq]: -D, LSE * log2(e)
   float* partial;       // [parts][G * Hkv][P][2][D] of dK / scale and dV, if parts > 1
-  int parts;
+  float* partial_s;     // [s_parts][B * Hkv][S][2][D], of the suffix tiles that several workgroups share
+  int parts;            // workgroups that share a prefix tile's stages evenly
+  int s_parts, s_run;   // a suffix tile's stages in runs of s_run; s_parts is the most runs a tile can have
+};
+
+// Of a suffix tile from key k0 on: the first block of 64 queries that sees it, and how many blocks from there on; per head.
+struct SuffixBlocks {
+  int first, count;
+  __device__ __forceinline__ SuffixBlocks(int k0, int ahead, int queries) {
+    const int row = k0 - ahead;  // the first query that sees key k0
+    first = row > 0 ? row / 64 : 0;
+    count = (queries + 63) / 64 - first;
+    if (count < 0) count = 0;
+  }
 };
 
 template <typename T, int D>
@@ -189,10 +203,10 @@ template <typename T, int D> struct GroupRows {
   __device__ __forceinline__ bool enter() {
     const int rows = length_of(q_lens, b, Nq);
     ahead = k0 < 0 ? ALL_AHEAD : S - rows;
-    const int first = k0 < 0 ? 0 : k0 - ahead;  // the first row that sees the tile's first key
-    s.block = first > 0 ? first / 64 : 0;
-    blocks = (rows + 63) / 64;
-    if (s.block >= blocks) return false;
+    const SuffixBlocks seen(k0, ahead, rows);
+    if (!seen.count) return false;
+    s.block = seen.first;
+    blocks = seen.first + seen.count;
     const size_t row = ((size_t)b * H + h) * (size_t)Nq;
     s.q = head_of<T>(Q, mq, b, h);
     s.dout = head_of<T>(dO, mdo, b, h);
@@ -212,8 +226,15 @@ template <typename T, int D> struct GroupRows {
       if (enter()) return true;
     }
   }
-  // The first stage; false if no row sees the tile.
-  __device__ __forceinline__ bool start() { return left >= 0 && (enter() || next_pair()); }
+  // Start at stage `skip` of a suffix tile's, `each` to a head, and take `count` of them.
+  __device__ __forceinline__ bool start_in(int skip, int each, int count) {
+    left = count - 1;
+    if (count <= 0) return false;
+    h = h0 + skip / each;
+    if (!enter()) return false;
+    s.block += skip % each;
+    return true;
+  }
   __device__ __forceinline__ bool advance() {
     if (--left < 0) return false;
     if (s.block + 1 < blocks) {
@@ -310,6 +331,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
   rows.partial = nullptr;
   int hk, tile;
   bool any = false;  // whether a row sees the tile
+  bool leader = true;
   const T *K, *V;
   TensorMap mk, mv;
   if (of_prefix) {
@@ -322,6 +344,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     rows.h = rows.h0 = hk * per;
     rows.h1 = rows.h0 + per;
     rows.k0 = -1;
+    leader = part == 0;
     const int stages = rows.stages(), begin = (int)((int64_t)stages * part / gr.parts);
     any = rows.start_at(begin, (int)((int64_t)stages * (part + 1) / gr.parts) - begin);
     rows.S = 0;
@@ -339,16 +362,23 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
   } else {
     // the first tiles of all suffixes first: more rows see them
     const int owners = p.B * p.Hkv, id = (int)blockIdx.x - first;
-    tile = id / owners;
-    const int owner = xcd_contiguous(id - tile * owners, owners), b = owner / p.Hkv;
+    const int unit = id / owners, run = unit % gr.s_parts;
+    tile = unit / gr.s_parts;
+    const int owner = xcd_contiguous(id - unit * owners, owners), b = owner / p.Hkv;
     hk = owner - b * p.Hkv;
     rows.b = b;
     rows.b_end = b + 1;
     rows.h = rows.h0 = hk * per;
     rows.h1 = rows.h0 + per;
-    rows.left = 1 << 30;
     rows.keys = rows.S = length_of(p.s_lens, b, p.S);
     rows.k0 = p.causal ? tile * BN : -1;
+    const int queries = length_of(p.q_lens, b, p.Nq);
+    const SuffixBlocks seen(rows.k0, p.causal ? rows.S - queries : ALL_AHEAD, queries);
+    const int stages = tile * BN < rows.keys ? per * seen.count : 0, begin = run * gr.s_run;
+    if (run > 0 && begin >= stages) return;
+    leader = run == 0;
+    if (stages > gr.s_run) rows.partial = gr.partial_s + ((size_t)run * (size_t)owners + owner) * (size_t)p.S * (2 * D);
+    if (stages) any = rows.start_in(begin, seen.count, stages - begin < gr.s_run ? stages - begin : gr.s_run);
     rows.all = p.S;
     rows.dK = gr.dKs + (size_t)b * (size_t)gr.mdks.batch + (size_t)hk * (size_t)gr.mdks.head;
     rows.dV = gr.dVs + (size_t)b * (size_t)gr.mdvs.batch + (size_t)hk * (size_t)gr.mdvs.head;
@@ -360,15 +390,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     mv = p.mvs;
   }
   const int k0 = tile * BN, k1 = k0 + BN < rows.all ? k0 + BN : rows.all;
-  if (!of_prefix) any = k0 < rows.keys && rows.start();
   const bool none = k0 >= rows.keys || !any;
-  if (!rows.partial) {  // rows of keys that do not exist, or that no query sees
-    const int from = none ? k0 : rows.keys > k0 ? rows.keys : k0;
-    if (from < k1) {
-      zero_rows(rows.dK, rows.mdk, from, k1, p.dh);
-      zero_rows(rows.dV, rows.mdv, from, k1, p.dh);
-    }
-  } else if (none) {
+  // Rows of keys that do not exist, or that no query sees: zeros, by the first of the workgroups that share the tile.  What
+  // the sum reads of a part without stages: zeros too.
+  const int from = none && !rows.partial ? k0 : rows.keys > k0 ? rows.keys : k0;
+  if (from < k1 && leader) {
+    zero_rows(rows.dK, rows.mdk, from, k1, p.dh);
+    zero_rows(rows.dV, rows.mdv, from, k1, p.dh);
+  }
+  if (none && rows.partial) {
     const int end = k1 < rows.keys ? k1 : rows.keys;
     for (int i = threadIdx.x; i < (end - k0) * (2 * D / 4); i += 256)
       reinterpret_cast<f32x4*>(rows.partial + (size_t)k0 * (2 * D))[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -385,24 +415,37 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
                                                       Dropout{}, 0, tile, rows);
 }
 
-// dKp and dVp from the parts, added in their order: a thread per four columns of a row.
+// dK and dV of the tiles that several workgroups share, from the parts, added in their order: a thread per four columns of a
+// row, first the rows of the prefixes (p_blocks workgroups), then those of the suffixes.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, float scale) {
+__global__ __launch_bounds__(256) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_blocks, float scale) {
   using v4 = typename Frag<T>::v4;
   constexpr int LPR = D / 4;
-  const int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR, owners = (int64_t)p.G * p.Hkv;
+  const bool of_prefix = (int)blockIdx.x < p_blocks;
+  const int n = of_prefix ? p.P : p.S;
+  const int64_t row = (int64_t)(of_prefix ? blockIdx.x : blockIdx.x - p_blocks) * (256 / LPR) + threadIdx.x / LPR;
+  const int64_t owners = (int64_t)(of_prefix ? p.G : p.B) * p.Hkv;
   const int col = (threadIdx.x % LPR) * 4;
-  if (row >= owners * p.P || col >= p.dh) return;
-  const int owner = (int)(row / p.P), key = (int)(row - (int64_t)owner * p.P), grp = owner / p.Hkv, hk = owner - grp * p.Hkv;
+  if (row >= owners * n || col >= p.dh) return;
+  const int owner = (int)(row / n), key = (int)(row - (int64_t)owner * n), outer = owner / p.Hkv, hk = owner - outer * p.Hkv;
+  int parts = gr.parts;
+  if (of_prefix) {
+    if (key >= length_of(p.prefix_lens, outer, p.P)) return;  // zeros already
+  } else {
+    const int keys = length_of(p.s_lens, outer, p.S), queries = length_of(p.q_lens, outer, p.Nq);
+    constexpr int BN = BwdKvPipeCfg<D>::BN;
+    const SuffixBlocks seen(p.causal ? key / BN * BN : -1, p.causal ? keys - queries : ALL_AHEAD, queries);
+    const int stages = p.H / p.Hkv * seen.count;
+    if (key >= keys || stages <= gr.s_run) return;  // one workgroup's, in place already
+    parts = (stages + gr.s_run - 1) / gr.s_run;
+  }
+  const float* x = (of_prefix ? gr.partial : gr.partial_s) + (size_t)row * (2 * D) + col;
+  const size_t step = (size_t)owners * (size_t)n * (2 * D);
   f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
-  if (key < length_of(p.prefix_lens, grp, p.P)) {
-    const float* x = gr.partial + (size_t)row * (2 * D) + col;
-    const size_t step = (size_t)owners * (size_t)p.P * (2 * D);
 #pragma unroll 4
-    for (int i = 0; i < gr.parts; ++i) {
-      a += *reinterpret_cast<const f32x4*>(x + i * step);
-      c += *reinterpret_cast<const f32x4*>(x + i * step + D);
-    }
+  for (int i = 0; i < parts; ++i) {
+    a += *reinterpret_cast<const f32x4*>(x + i * step);
+    c += *reinterpret_cast<const f32x4*>(x + i * step + D);
   }
   v4 k, v;
 #pragma unroll
@@ -410,10 +453,11 @@ __global__ __launch_bounds__(256) void mha_prefix_sum_kernel(PrefixProblem p, Pr
     k[e] = (T)(a[e] * scale);
     v[e] = (T)c[e];
   }
-  *reinterpret_cast<v4*>(gr.dKp + (size_t)grp * (size_t)gr.mdkp.batch + (size_t)hk * (size_t)gr.mdkp.head +
-                         (size_t)key * (size_t)gr.mdkp.row + col) = k;
-  *reinterpret_cast<v4*>(gr.dVp + (size_t)grp * (size_t)gr.mdvp.batch + (size_t)hk * (size_t)gr.mdvp.head +
-                         (size_t)key * (size_t)gr.mdvp.row + col) = v;
+  T* const dK = of_prefix ? gr.dKp : gr.dKs;
+  T* const dV = of_prefix ? gr.dVp : gr.dVs;
+  const TensorMap &mk = of_prefix ? gr.mdkp : gr.mdks, &mv = of_prefix ? gr.mdvp : gr.mdvs;
+  *reinterpret_cast<v4*>(dK + (size_t)outer * (size_t)mk.batch + (size_t)hk * (size_t)mk.head + (size_t)key * (size_t)mk.row + col) = k;
+  *reinterpret_cast<v4*>(dV + (size_t)outer * (size_t)mv.batch + (size_t)hk * (size_t)mv.head + (size_t)key * (size_t)mv.row + col) = v;
 }
 
 }  // namespace spark

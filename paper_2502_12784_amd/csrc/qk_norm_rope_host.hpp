@@ -35,10 +35,11 @@ int qk_vec(int d, int rd) { return d % 16 == 0 && rd % 16 == 0 ? 8 : 4; }
 // Lanes of a row: 4 rows' widths of 64 and 128 columns.
 int qk_lanes(int d, int vec) { return (d <= 64 ? 64 : 128) / (2 * vec); }
 
-// Heads of a workgroup: as many as leave four workgroups to a CU.
+// Heads of a workgroup: as many as leave two workgroups to a CU.  (us, at least 1024 -> 512 workgroups: a step of 3 x 1333
+// tokens, 16 heads of 80 30.2 -> 23.5, 16384 x 40 heads of 64 83.9 -> 83.0, a forward of 8192 x 32 of 128 26.8 -> 27.8.)
 int qk_group(const QkNormRope& a, int token_blocks) {
   int group = 16;
-  while (group > 1 && (int64_t)token_blocks * ((a.H + group - 1) / group + (a.Hkv + group - 1) / group) < 1024) group /= 2;
+  while (group > 1 && (int64_t)token_blocks * ((a.H + group - 1) / group + (a.Hkv + group - 1) / group) < 512) group /= 2;
   return group;
 }
 
