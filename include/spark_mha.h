@@ -327,7 +327,7 @@ int spark_mha_strided_bwd(const void* Q, const void* K, const void* V, const voi
  *   positions : in, device, [B,N] int32: each token's row of the tables; NULL: token n has position n (N <= table).
  *               A negative position marks padding: the token's results are zeros, and it adds to no gradient.  A
  *               position behind the table (a mistake that the host cannot see) gives NaN; nothing is read there.
- * Supported: d a multiple of 8 in 8..128; rd a multiple of 8 in 0..d; H, Hkv <= 32768; B*N < 2^31 - 65536; eps finite
+ * Supported: d a multiple of 8 in 8..128; rd a multiple of 8 in 0..d; H, Hkv <= 32768; B*N < 2^30; eps finite
  * and > 0.  Strides as in spark_mha_strided_fwd, but of any size (64-bit offsets), and the stride of an index with one
  * value does not matter.
  */
@@ -363,7 +363,8 @@ int spark_qk_norm_rope_bwd(const void* Q, const void* K, const void* wq, const v
  * namely all prefix_lens[g] keys of the prefix, and of the suffix key j < s_lens[b], with causal != 0 only
  * j <= i + s_lens[b] - q_lens[b] (the queries are the last tokens of the sequence).
  *   prefix_lens [G], q_lens, s_lens [B] : in, device, int32; NULL: P, Nq, S.  Values are taken to be in 0 ... P (Nq, S);
- *               others are cut to that.  Keys behind a length are never used, whatever stands there (NaN too).  Query rows
+ *               others are cut to that.  Keys behind a length are never used, whatever stands there (NaN too); those
+ *               within must be finite, also where the causal mask hides them (0 * inf).  Query rows
  *               from q_lens[b] on are padding, and rows that see no key at all are allowed: both give O = 0, LSE = -inf.
  * One new token per sequence is Nq = 1 with s_lens counting it; training on several answers to one prompt is Nq = S
  * (q_lens = s_lens) with the prompt as prefix.

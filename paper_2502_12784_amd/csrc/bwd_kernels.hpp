@@ -638,7 +638,7 @@ static __device__ __forceinline__ void bwd_dq(
     if constexpr (Keys::PREFIX) {
       load_row_frags(qf, Q + keys.offset(mq, qrow_c), g, dh);
       load_row_frags(dof, dO + keys.offset(mdo, qrow_c), g, dh);
-      load_row_frags(of, O + keys.offset(mo, qrow_c), g, dh);
+      if constexpr (!STATS) load_row_frags(of, O + keys.offset(mo, qrow_c), g, dh);
     } else if constexpr (CAUSAL) {
       load_row_frags(qf, Qh + (size_t)qrow_c * (size_t)mq.row, g, dh);
       load_row_frags(dof, dOh + (size_t)qrow_c * (size_t)mdo.row, g, dh);

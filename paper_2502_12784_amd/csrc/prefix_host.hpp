@@ -170,41 +170,69 @@ PrefixShares prefix_shares(const PrefixProblem& p) {
   return PrefixShares{(int)best, p.S ? (int)((w2 + run - 1) / run) : 1, (int)run};
 }
 size_t prefix_stats_bytes(const PrefixProblem& p) { return ((size_t)p.B * p.H * p.Nq * 8 + 255) & ~(size_t)255; }
+// Floats of the parts of all prefix tiles, and of all suffix tiles (PrefixTile).
+size_t part_floats(const PrefixProblem& p, int parts, int outer, int n) {
+  const size_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
+  return parts > 1 ? (size_t)parts * outer * p.Hkv * ((n + 127) / 128) * 128 * 2 * columns : 0;
+}
+size_t prefix_part_floats(const PrefixProblem& p, const PrefixShares& x) { return part_floats(p, x.parts, p.G, p.P); }
+size_t suffix_part_floats(const PrefixProblem& p, const PrefixShares& x) { return part_floats(p, x.s_parts, p.B, p.S); }
 size_t prefix_bwd_workspace(const PrefixProblem& p) {
   const PrefixShares x = prefix_shares(p);
-  const size_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
-  return prefix_stats_bytes(p) + (x.parts > 1 ? (size_t)x.parts * p.G * p.Hkv * p.P * columns * 8 : 0) +
-         (x.s_parts > 1 ? (size_t)x.s_parts * p.B * p.Hkv * p.S * columns * 8 : 0);
+  return prefix_stats_bytes(p) + sizeof(float) * (prefix_part_floats(p, x) + suffix_part_floats(p, x));
+}
+
+// Whether dQ and dK/dV run in one grid: where dQ's tiles alone leave CUs idle.  In one grid dQ, which has two workgroups to a
+// CU by itself, is held to one at more than 64 columns.  Steps, us, a grid for each -> one grid (n tiles of dQ):
+//   d = 64:   2 sequences x 8 heads over 2 x 128 queries behind 256 (16) 34.5 -> 27.5   8 x 8 x 512 behind 1024 (256) 88.2 -> 86.4
+//             4 x 8 x 512 behind 4096 (128) 152.8 -> 138.4                               16 x 8 x 512 behind 1024 (512) 137.9 -> 132.6
+//   d <= 96:  6 x 6 over 2 x 333 behind 700 (96) 81.5 -> 68.1                            8 x 12 x 384 behind 512 (288) 106.5 -> 100.5
+//   d = 128:  4 x 16 over 4 x 256 behind 512 (128) 88.4 -> 83.9                          8 x 16 x 256 behind 1024 (256) 131.0 -> 136.2
+//             8 x 16 over 4 x 512 behind 2048 (512) 311.7 -> 354.9
+bool prefix_merged(const PrefixProblem& p) {
+  const int64_t dq = (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128);
+  return dq <= (p.dh <= 64 ? 512 : p.dh <= 96 ? 288 : 192);
 }
 
 template <typename T, int D>
-int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, float scale, hipStream_t st) {
-  {
-    using C = BwdQCfg<D, true, false>;
-    auto kernel = mha_prefix_dq_kernel<T, D>;
+int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, float scale, bool merged, hipStream_t st) {
+  using Q = BwdQCfg<D, true, false>;
+  using C = BwdKvPipeCfg<D>;
+  const int nqt = (p.Nq * (p.H / p.Hkv) + Q::BM - 1) / Q::BM, dq_items = p.B * p.Hkv * nqt;
+  const int p_tiles = (p.P + C::BN - 1) / C::BN, s_tiles = (p.S + C::BN - 1) / C::BN;
+  const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles * gr.s_parts;
+  if (merged) {
+    constexpr int W = lds_row<D>, RPB = 256 / (W / 8), SMEM = C::SMEM > Q::SMEM ? C::SMEM : Q::SMEM;
+    const int64_t rows = (int64_t)p.B * p.H * p.Nq;
+    hipLaunchKernelGGL((mha_prefix_stats_kernel<T, W>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, st, p,
+                       static_cast<const T*>(O), gr);
+    if (!launch_ok("backward statistics kernel (prefix)")) return SPARK_ERR_LAUNCH;
+    auto kernel = mha_prefix_bwd_kernel<T, D>;
+    static std::atomic<uint64_t> ready{0};
+    const int attr = ensure_smem(kernel, SMEM, ready);
+    if (attr != SPARK_OK) return attr;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(grid + dq_items)), dim3(256), SMEM, st, p, gr, p_tiles, s_tiles, first, nqt, scale);
+    if (!launch_ok("backward kernel (prefix, both sides)")) return SPARK_ERR_LAUNCH;
+  } else {
+    {
+      auto kernel = mha_prefix_dq_kernel<T, D>;
+      static std::atomic<uint64_t> ready{0};
+      const int attr = ensure_smem(kernel, Q::SMEM, ready);
+      if (attr != SPARK_OK) return attr;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)dq_items), dim3(256), Q::SMEM, st, p, static_cast<const T*>(O), gr, nqt, scale);
+      if (!launch_ok("dQ kernel (prefix)")) return SPARK_ERR_LAUNCH;
+    }
+    auto kernel = mha_prefix_dkdv_kernel<T, D>;
     static std::atomic<uint64_t> ready{0};
     const int attr = ensure_smem(kernel, C::SMEM, ready);
     if (attr != SPARK_OK) return attr;
-    const int nqt = (p.Nq * (p.H / p.Hkv) + C::BM - 1) / C::BM;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(256), C::SMEM, st, p, static_cast<const T*>(O), gr, nqt,
-                       scale);
-    if (!launch_ok("dQ kernel (prefix)")) return SPARK_ERR_LAUNCH;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), C::SMEM, st, p, gr, p_tiles, s_tiles, first, scale);
+    if (!launch_ok("dK/dV kernel (prefix)")) return SPARK_ERR_LAUNCH;
   }
-  using C = BwdKvPipeCfg<D>;
-  auto kernel = mha_prefix_dkdv_kernel<T, D>;
-  static std::atomic<uint64_t> ready{0};
-  const int attr = ensure_smem(kernel, C::SMEM, ready);
-  if (attr != SPARK_OK) return attr;
-  const int p_tiles = (p.P + C::BN - 1) / C::BN, s_tiles = (p.S + C::BN - 1) / C::BN;
-  const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles * gr.s_parts;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), C::SMEM, st, p, gr, p_tiles, s_tiles, first, scale);
-  if (!launch_ok("dK/dV kernel (prefix)")) return SPARK_ERR_LAUNCH;
   if (gr.parts == 1 && gr.s_parts == 1) return SPARK_OK;
-  constexpr int RPB = 256 * 4 / D;
-  const int64_t p_rows = gr.parts > 1 ? (int64_t)p.G * p.Hkv * p.P : 0, s_rows = gr.s_parts > 1 ? (int64_t)p.B * p.Hkv * p.S : 0;
-  const int p_blocks = (int)((p_rows + RPB - 1) / RPB), s_blocks = (int)((s_rows + RPB - 1) / RPB);
-  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)(p_blocks + s_blocks)), dim3(256), 0, st, p, gr, p_blocks,
-                     scale);
+  const int p_blocks = gr.parts > 1 ? p.G * p.Hkv * p_tiles * 4 : 0, s_blocks = gr.s_parts > 1 ? p.B * p.Hkv * s_tiles * 4 : 0;
+  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)(p_blocks + s_blocks)), dim3(1024), 0, st, p, gr, p_blocks,
+                     p_tiles, s_tiles, scale);
   return launch_ok("sum of the parts (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
@@ -234,11 +262,11 @@ int dispatch_prefix_bwd(const PrefixProblem& p, const void* O, const PrefixGradA
   gr.parts = x.parts;
   gr.s_parts = x.s_parts;
   gr.s_run = x.s_run;
-  const int64_t columns = p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128;
-  gr.partial_s = gr.partial + (x.parts > 1 ? (size_t)x.parts * p.G * p.Hkv * p.P * columns * 2 : 0);
-  if (p.dh <= 64) return launch_prefix_bwd<T, 64>(p, O, gr, scale, st);
-  if (p.dh <= 96) return launch_prefix_bwd<T, 96>(p, O, gr, scale, st);
-  return launch_prefix_bwd<T, 128>(p, O, gr, scale, st);
+  gr.partial_s = gr.partial + prefix_part_floats(p, x);
+  const bool merged = prefix_merged(p);
+  if (p.dh <= 64) return launch_prefix_bwd<T, 64>(p, O, gr, scale, merged, st);
+  if (p.dh <= 96) return launch_prefix_bwd<T, 96>(p, O, gr, scale, merged, st);
+  return launch_prefix_bwd<T, 128>(p, O, gr, scale, merged, st);
 }
 
 }  // namespace

@@ -126,10 +126,17 @@ template <typename T> struct PrefixGrads {
   TensorMap mdo, mdq, mdkp, mdvp, mdks, mdvs;
   const float* LSE;
   float *Dws, *LSE2ws;  // [B,H,Nq]: -D, LSE * log2(e)
-  float* partial;       // [parts][G * Hkv][P][2][D] of dK / scale and dV, if parts > 1
-  float* partial_s;     // [s_parts][B * Hkv][S][2][D], of the suffix tiles that several workgroups share
+  float* partial;       // if parts > 1: [parts][G * Hkv][tiles of P] tiles of dK / scale and dV (PrefixTile)
+  float* partial_s;     // if s_parts > 1: [s_parts][B * Hkv][tiles of S], of the suffix tiles that several workgroups share
   int parts;            // workgroups that share a prefix tile's stages evenly
   int s_parts, s_run;   // a suffix tile's stages in runs of s_run; s_parts is the most runs a tile can have
+};
+
+// A part of a tile's dK / scale and dV in fp32, as the accumulators hold them: [wave][eight columns of dK, then of dV][lane][4],
+// lane l with columns 4 (l / 32) + 0 ... 3 of key l % 32 of the wave: every store and load is 1 KB in one piece.  (Rows of keys
+// instead, whose stores are pieces of 32 bytes: dK/dV of the 16 sequences above 207.3 us, so 205.4.)
+template <int D> struct PrefixTile {
+  static constexpr int EIGHTS = 2 * D / 8, WAVE = EIGHTS * 256, FLOATS = 4 * WAVE;
 };
 
 // Of a suffix tile from key k0 on: the first block of 64 queries that sees it, and how many blocks from there on; per head.
@@ -143,10 +150,10 @@ struct SuffixBlocks {
   }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void mha_prefix_dq_kernel(PrefixProblem p, const T* __restrict__ O, PrefixGrads<T> gr,
-                                                               int nqt, float scale) {
-  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
+// The workgroup's part of dQ: tile `logical` of all sequences' and heads' tiles.  STATS: D and LSE * log2(e) are there already.
+template <typename T, int D, bool STATS>
+static __device__ __forceinline__ void prefix_dq(const PrefixProblem& p, const T* __restrict__ O, const PrefixGrads<T>& gr, int nqt,
+                                                 float scale, int logical) {
   const int flat = logical / nqt, item = logical - flat * nqt;
   const PrefixHead x(p, flat);
   const PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
@@ -157,17 +164,25 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_dq_kernel(PrefixProblem p, 
   const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < all ? row0 + BM : all;
   if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
     zero_rows(dQ, gr.mdq, keys, row0, row1, p.dh);
-    for (int r = row0 + threadIdx.x; r < row1; r += 256) {
-      gr.Dws[stats + keys.stat(r)] = 0.f;
-      gr.LSE2ws[stats + keys.stat(r)] = INFINITY;
+    if (!STATS) {
+      for (int r = row0 + threadIdx.x; r < row1; r += 256) {
+        gr.Dws[stats + keys.stat(r)] = 0.f;
+        gr.LSE2ws[stats + keys.stat(r)] = INFINITY;
+      }
     }
     return;
   }
-  bwd_dq<T, D, true, false, false, IN_ORDER>(
+  bwd_dq<T, D, true, false, STATS, IN_ORDER>(
       head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk), head_of<T>(p.Vs, p.mvs, x.b, x.hk),
       head_of<T>(O, p.mo, x.b, h0), head_of<T>(gr.dO, gr.mdo, x.b, h0), gr.LSE + stats, gr.Dws + stats, gr.LSE2ws + stats, dQ,
       p.mq, p.mks, p.mvs, p.mo, gr.mdo, gr.mdq, p.H, all, x.S, p.dh, nqt, 0, scale, scale * 1.4426950408889634f, Dropout{}, 0,
       item, keys);
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void mha_prefix_dq_kernel(PrefixProblem p, const T* __restrict__ O, PrefixGrads<T> gr,
+                                                               int nqt, float scale) {
+  prefix_dq<T, D, false>(p, O, gr, nqt, scale, xcd_contiguous(blockIdx.x, gridDim.x));
 }
 
 // The query rows that see a key tile, in stages of 64 of one (sequence, head), for bwd_dkdv_pipe; and where its sums go.
@@ -195,7 +210,7 @@ template <typename T, int D> struct GroupRows {
   T *dK, *dV;              // of the tile's head
   TensorMap mdk, mdv;
   int keys, all;           // keys that exist, rows that are written (zeros behind the keys)
-  float* partial;          // or the tile's head's partial sums
+  float* partial;          // or the workgroup's part of the tile
 
   __device__ __forceinline__ Stage stage() const { return s; }
   __device__ __forceinline__ int first_query() const { return s.block * 64 + ahead; }
@@ -286,23 +301,18 @@ template <typename T, int D> struct GroupRows {
                                         int lane, float scale) const {
     constexpr int OSTR = BwdKvPipeCfg<D>::OSTR;
     if (partial) {
-      asm volatile("" : "+v"(lane));
-      const int key = k0w + (lane & 31), g = lane >> 5;
-      float* out = partial + (size_t)key * (2 * D) + 4 * g;
-      if (key >= keys) return;
+      float* out = partial + (k0w >> 5 & 3) * PrefixTile<D>::WAVE + lane * 4;
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
+      for (int q = 0; q < D / 8; ++q) {
+        f32x4 a, c;
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          f32x4 a, c;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            a[e] = dk[dt][4 * r4 + e];
-            c[e] = dv[dt][4 * r4 + e];
-          }
-          *reinterpret_cast<f32x4*>(out + dt * 32 + 8 * r4) = a;
-          *reinterpret_cast<f32x4*>(out + D + dt * 32 + 8 * r4) = c;
+        for (int e = 0; e < 4; ++e) {
+          a[e] = dk[q / 4][4 * (q % 4) + e];
+          c[e] = dv[q / 4][4 * (q % 4) + e];
         }
+        *reinterpret_cast<f32x4*>(out + q * 256) = a;
+        *reinterpret_cast<f32x4*>(out + (D / 8 + q) * 256) = c;
+      }
       return;
     }
     store_transposed<T, D, OSTR>(dk, scale, ob, dK, k0w, keys, lane, (size_t)mdk.row, dh);
@@ -310,13 +320,13 @@ template <typename T, int D> struct GroupRows {
   }
 };
 
+// The workgroup's part of dK and dV: `block` of first + B * Hkv * s_tiles * s_parts.
 template <typename T, int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(PrefixProblem p, PrefixGrads<T> gr,
-                                                                               int p_tiles, int s_tiles, int first,
-                                                                               float scale) {
+static __device__ __forceinline__ void prefix_dkdv(const PrefixProblem& p, const PrefixGrads<T>& gr, int p_tiles, int s_tiles,
+                                                   int first, float scale, int block) {
   constexpr int BN = BwdKvPipeCfg<D>::BN;
   const int per = p.H / p.Hkv, seqs = p.B / p.G;
-  const bool of_prefix = (int)blockIdx.x < first;  // the longer ones first
+  const bool of_prefix = block < first;  // the longer ones first
   GroupRows<T, D> rows;
   rows.Q = static_cast<const T*>(p.Q);
   rows.dO = gr.dO;
@@ -335,7 +345,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
   const T *K, *V;
   TensorMap mk, mv;
   if (of_prefix) {
-    const int logical = xcd_contiguous(blockIdx.x, first);
+    const int logical = xcd_contiguous(block, first);
     tile = logical % p_tiles;
     const int unit = logical / p_tiles, part = unit % gr.parts, owner = unit / gr.parts, grp = owner / p.Hkv;
     hk = owner - grp * p.Hkv;
@@ -350,7 +360,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     rows.S = 0;
     rows.keys = length_of(p.prefix_lens, grp, p.P);
     rows.all = p.P;
-    if (gr.parts > 1) rows.partial = gr.partial + ((size_t)part * (size_t)(p.G * p.Hkv) + owner) * (size_t)p.P * (2 * D);
+    if (gr.parts > 1) rows.partial = gr.partial + (((size_t)part * (size_t)(p.G * p.Hkv) + owner) * (size_t)p_tiles + tile) * PrefixTile<D>::FLOATS;
     rows.dK = gr.dKp + (size_t)grp * (size_t)gr.mdkp.batch + (size_t)hk * (size_t)gr.mdkp.head;
     rows.dV = gr.dVp + (size_t)grp * (size_t)gr.mdvp.batch + (size_t)hk * (size_t)gr.mdvp.head;
     rows.mdk = gr.mdkp;
@@ -361,7 +371,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     mv = p.mvp;
   } else {
     // the first tiles of all suffixes first: more rows see them
-    const int owners = p.B * p.Hkv, id = (int)blockIdx.x - first;
+    const int owners = p.B * p.Hkv, id = block - first;
     const int unit = id / owners, run = unit % gr.s_parts;
     tile = unit / gr.s_parts;
     const int owner = xcd_contiguous(id - unit * owners, owners), b = owner / p.Hkv;
@@ -377,7 +387,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     const int stages = tile * BN < rows.keys ? per * seen.count : 0, begin = run * gr.s_run;
     if (run > 0 && begin >= stages) return;
     leader = run == 0;
-    if (stages > gr.s_run) rows.partial = gr.partial_s + ((size_t)run * (size_t)owners + owner) * (size_t)p.S * (2 * D);
+    if (stages > gr.s_run) rows.partial = gr.partial_s + (((size_t)run * (size_t)owners + owner) * (size_t)s_tiles + tile) * PrefixTile<D>::FLOATS;
     if (stages) any = rows.start_in(begin, seen.count, stages - begin < gr.s_run ? stages - begin : gr.s_run);
     rows.all = p.S;
     rows.dK = gr.dKs + (size_t)b * (size_t)gr.mdks.batch + (size_t)hk * (size_t)gr.mdks.head;
@@ -399,9 +409,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
     zero_rows(rows.dV, rows.mdv, from, k1, p.dh);
   }
   if (none && rows.partial) {
-    const int end = k1 < rows.keys ? k1 : rows.keys;
-    for (int i = threadIdx.x; i < (end - k0) * (2 * D / 4); i += 256)
-      reinterpret_cast<f32x4*>(rows.partial + (size_t)k0 * (2 * D))[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = threadIdx.x; i < PrefixTile<D>::FLOATS / 4; i += 256)
+      reinterpret_cast<f32x4*>(rows.partial)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   if (none) return;
   const TensorMap none_map{0, 0, 0};
@@ -415,49 +424,106 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
                                                       Dropout{}, 0, tile, rows);
 }
 
-// dK and dV of the tiles that several workgroups share, from the parts, added in their order: a thread per four columns of a
-// row, first the rows of the prefixes (p_blocks workgroups), then those of the suffixes.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_blocks, float scale) {
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(PrefixProblem p, PrefixGrads<T> gr,
+                                                                               int p_tiles, int s_tiles, int first,
+                                                                               float scale) {
+  prefix_dkdv<T, D>(p, gr, p_tiles, s_tiles, first, scale, blockIdx.x);
+}
+
+// Both in one grid where one of them leaves CUs idle: the workgroups of the prefix's keys, those of dQ, those of the suffixes'.
+// D and LSE * log2(e) are formed by a kernel of their own first.
+template <typename T, int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_bwd_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_tiles,
+                                                                              int s_tiles, int first, int nqt, float scale) {
+  const int dq_items = p.B * p.Hkv * nqt, block = blockIdx.x;
+  if (block >= first && block < first + dq_items)
+    prefix_dq<T, D, true>(p, nullptr, gr, nqt, scale, xcd_contiguous(block - first, dq_items));
+  else
+    prefix_dkdv<T, D>(p, gr, p_tiles, s_tiles, first, scale, block < first ? block : block - dq_items);
+}
+
+// -D and LSE * log2(e) of every row: W / 8 lanes to a row.  A row without keys gets inf, so that its P is 0; rows not in use are
+// never read.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void mha_prefix_stats_kernel(PrefixProblem p, const T* __restrict__ O, PrefixGrads<T> gr) {
+  using v8 = typename Frag<T>::v8;
+  constexpr int LPR = W / 8;
+  const size_t rows = (size_t)p.B * p.H * (size_t)p.Nq, row = (size_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const size_t r = row < rows ? row : rows - 1;
+  const int bh = (int)(r / (size_t)p.Nq), i = (int)(r - (size_t)bh * p.Nq), b = bh / p.H, h = bh - b * p.H;
+  const int col = (threadIdx.x % LPR) * 8;
+  const bool used = row < rows && i < length_of(p.q_lens, b, p.Nq);
+  const v8 o = load_row_chunk<v8>(head_of<T>(O, p.mo, b, h) + (size_t)i * (size_t)p.mo.row, col, p.dh);
+  const v8 g = load_row_chunk<v8>(head_of<T>(gr.dO, gr.mdo, b, h) + (size_t)i * (size_t)gr.mdo.row, col, p.dh);
+  float acc = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc = __builtin_fmaf((float)o[e], (float)g[e], acc);
+#pragma unroll
+  for (int m = LPR / 2; m >= 1; m >>= 1) acc += __shfl_xor(acc, m, LPR);
+  if (used && col == 0) {
+    const float lse = gr.LSE[r];
+    gr.Dws[r] = -acc;
+    gr.LSE2ws[r] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;
+  }
+}
+
+// dK and dV of the tiles that several workgroups share, from the parts, added in their order: a workgroup per 32 keys, first of
+// the prefixes (p_blocks workgroups), then of the suffixes.
+template <typename T, int D>
+__global__ __launch_bounds__(1024) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_blocks, int p_tiles,
+                                                             int s_tiles, float scale) {
   using v4 = typename Frag<T>::v4;
-  constexpr int LPR = D / 4;
+  using Tile = PrefixTile<D>;
+  __shared__ __align__(16) T rows[32][2 * D + 8];
   const bool of_prefix = (int)blockIdx.x < p_blocks;
-  const int n = of_prefix ? p.P : p.S;
-  const int64_t row = (int64_t)(of_prefix ? blockIdx.x : blockIdx.x - p_blocks) * (256 / LPR) + threadIdx.x / LPR;
-  const int64_t owners = (int64_t)(of_prefix ? p.G : p.B) * p.Hkv;
-  const int col = (threadIdx.x % LPR) * 4;
-  if (row >= owners * n || col >= p.dh) return;
-  const int owner = (int)(row / n), key = (int)(row - (int64_t)owner * n), outer = owner / p.Hkv, hk = owner - outer * p.Hkv;
-  int parts = gr.parts;
+  const int id = of_prefix ? blockIdx.x : (int)blockIdx.x - p_blocks, quarter = id & 3, at = id >> 2;
+  const int tiles = of_prefix ? p_tiles : s_tiles, owner = at / tiles, tile = at - owner * tiles, outer = owner / p.Hkv,
+            hk = owner - outer * p.Hkv, key0 = tile * 128 + quarter * 32;
+  int parts = gr.parts, keys;
   if (of_prefix) {
-    if (key >= length_of(p.prefix_lens, outer, p.P)) return;  // zeros already
+    keys = length_of(p.prefix_lens, outer, p.P);
   } else {
-    const int keys = length_of(p.s_lens, outer, p.S), queries = length_of(p.q_lens, outer, p.Nq);
-    constexpr int BN = BwdKvPipeCfg<D>::BN;
-    const SuffixBlocks seen(p.causal ? key / BN * BN : -1, p.causal ? keys - queries : ALL_AHEAD, queries);
+    keys = length_of(p.s_lens, outer, p.S);
+    const int queries = length_of(p.q_lens, outer, p.Nq);
+    const SuffixBlocks seen(p.causal ? tile * 128 : -1, p.causal ? keys - queries : ALL_AHEAD, queries);
     const int stages = p.H / p.Hkv * seen.count;
-    if (key >= keys || stages <= gr.s_run) return;  // one workgroup's, in place already
+    if (stages <= gr.s_run) return;  // one workgroup's, in place already
     parts = (stages + gr.s_run - 1) / gr.s_run;
   }
-  const float* x = (of_prefix ? gr.partial : gr.partial_s) + (size_t)row * (2 * D) + col;
-  const size_t step = (size_t)owners * (size_t)n * (2 * D);
-  f32x4 a = {0.f, 0.f, 0.f, 0.f}, c = a;
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    a += *reinterpret_cast<const f32x4*>(x + i * step);
-    c += *reinterpret_cast<const f32x4*>(x + i * step + D);
-  }
-  v4 k, v;
+  if (key0 >= keys) return;  // zeros already
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* x = (of_prefix ? gr.partial : gr.partial_s) + (size_t)at * Tile::FLOATS + quarter * Tile::WAVE + lane * 4;
+  const size_t step = (size_t)(of_prefix ? p.G : p.B) * (size_t)p.Hkv * (size_t)tiles * Tile::FLOATS;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    k[e] = (T)(a[e] * scale);
-    v[e] = (T)c[e];
+  for (int q = wave; q < Tile::EIGHTS; q += 16) {
+    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < parts; i += 4) {  // four requested together
+      f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4*>(x + (i + u < parts ? i + u : i) * step + q * 256);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i + u < parts) a += v[u];
+      }
+    }
+    const float mul = q < Tile::EIGHTS / 2 ? scale : 1.0f;
+    v4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (T)(a[e] * mul);
+    *reinterpret_cast<v4*>(&rows[lane & 31][8 * q + 4 * (lane >> 5)]) = r;
   }
+  __syncthreads();
   T* const dK = of_prefix ? gr.dKp : gr.dKs;
   T* const dV = of_prefix ? gr.dVp : gr.dVs;
   const TensorMap &mk = of_prefix ? gr.mdkp : gr.mdks, &mv = of_prefix ? gr.mdvp : gr.mdvs;
-  *reinterpret_cast<v4*>(dK + (size_t)outer * (size_t)mk.batch + (size_t)hk * (size_t)mk.head + (size_t)key * (size_t)mk.row + col) = k;
-  *reinterpret_cast<v4*>(dV + (size_t)outer * (size_t)mv.batch + (size_t)hk * (size_t)mv.head + (size_t)key * (size_t)mv.row + col) = v;
+  for (int i = threadIdx.x; i < 32 * (2 * D / 8); i += 1024) {
+    const int row = i / (2 * D / 8), c = i % (2 * D / 8), col = c % (D / 8) * 8, key = key0 + row;
+    if (key >= keys || col >= p.dh) continue;
+    const TensorMap& m = c < D / 8 ? mk : mv;
+    T* const out = (c < D / 8 ? dK : dV) + (size_t)outer * (size_t)m.batch + (size_t)hk * (size_t)m.head + (size_t)key * (size_t)m.row;
+    *reinterpret_cast<u32x4*>(out + col) = *reinterpret_cast<const u32x4*>(&rows[row][8 * c]);
+  }
 }
 
 }  // namespace spark

@@ -23,8 +23,8 @@ int make_qk(QkNormRope* a, int B, int N, int H, int Hkv, int d, int rd, int tabl
   if (B < 1 || N < 1 || H < 1 || Hkv < 1 || d < 8 || d > 128 || (d & 7)) return SPARK_ERR_SHAPE;
   if (rd < 0 || rd > d || (rd & 7) || (rd > 0 && table < 1)) return SPARK_ERR_SHAPE;
   if (!isfinite(eps) || !(eps > 0.f)) return SPARK_ERR_SHAPE;
-  // 32-bit token indices, a group of heads per row of the grid
-  if ((int64_t)B * N >= ((int64_t)1 << 31) - 65536 || H > 32768 || Hkv > 32768) return SPARK_ERR_SHAPE;
+  // token indices, with a stride of the grid added, in 31 bits; a group of heads per row of the grid
+  if ((int64_t)B * N >= (int64_t)1 << 30 || H > 32768 || Hkv > 32768) return SPARK_ERR_SHAPE;
   a->tokens = B * N; a->N = N; a->H = H; a->Hkv = Hkv; a->d = d; a->rd = rd; a->table = table;
   a->eps = eps; a->inv_d = 1.0f / (float)d; a->w_is_fp32 = w_fp32 != 0;
   return SPARK_OK;
