@@ -48,20 +48,34 @@ int launch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, float scale, 
   return launch_ok("forward kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
-// Workgroups of 8 waves (256 rows, one per CU) instead of 4: the rule of wide_workgroups in spark_mha.hip, for the same loop.
+// Workgroups of 8 waves (256 rows, one per CU) instead of 4: the rule of wide_workgroups in spark_mha.hip, for the same loop;
+// not where the last of few tiles would stay half empty (us, 64 sequences x 32 heads over 8 x 16 queries behind 2048, one
+// half tile each: 118 in wide ones, 71).
 bool prefix_wide(const PrefixProblem& p) {
   const int64_t rows = (int64_t)p.Nq * (p.H / p.Hkv), owners = (int64_t)p.B * p.Hkv;
   const int64_t wide = owners * ((rows + 255) / 256), narrow = owners * ((rows + 127) / 128);
-  return (int64_t)p.P + p.S >= 2048 && (wide >= 512 || narrow >= 896 || (wide <= 256 && narrow > 256));
+  return (int64_t)p.P + p.S >= 2048 && 7 * wide <= 4 * narrow && (wide >= 512 || narrow >= 896 || (wide <= 256 && narrow > 256));
 }
 
-// Whether the rows are packed and the keys go to several workgroups in runs (prefix_parts.hpp).
+// Whether rows are packed across sequences and the keys go to several workgroups in runs (prefix_parts.hpp), or every tile of a
+// sequence's rows walks all its keys by itself.  The latter for up to three tiles of keys, where a second kernel costs more than
+// anything saves, and where its tiles fill the chip and are well filled themselves.  Forward, us, d = 128 but where said, packed
+// / by themselves:
+//   32 sequences x 16 heads x 1 behind 64 / 128 / 192 / 256 keys   14.0 / 10.5   13.9 / 11.8   13.9 / 13.3   13.8 / 14.7
+//   2 x 4 x 1, d = 64, behind 64 / 128 / 192 / 256                  7.0 / 6.3   7.2 / 7.0   7.3 / 7.7   7.5 / 8.5
+//   rows of a tile in use, half: 32 x 16 x 64 behind 1024 42.5 / 36.7, d = 64 28.4 / 24.9; 64 x 32 over 8 x 16 behind 2048 62.6 / 70.6;
+//   a third: 64 x 16 x 48 behind 2048 82.8 / 125, 32 x 16 x 40 behind 1024 32.4 / 35.4; a quarter: 64 x 16 x 32 behind 2048 57 / 119;
+//   three quarters: 16 x 16 x 96 behind 1024 36.2 / 27.0, 16 x 64 over 16 x 24 behind 2048 47.5 / 40.6
+//   few tiles (n): 2 x 16 x 256 behind 4096 (64) 35 / 73, 4 x 16 x 256 (128) 55 / 74, 8 x 16 x 160 behind 2048 (256) 46.0 / 43.6
 bool prefix_packed(const PrefixProblem& p) {
-  return p.Nq <= 32 || (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128) < 256;
+  const int64_t rows = (int64_t)p.Nq * (p.H / p.Hkv), tiles = (rows + 127) / 128;
+  if (((int64_t)p.P + 63) / 64 + ((int64_t)p.S + 63) / 64 <= 3) return false;
+  if (p.B * (int64_t)p.Hkv * tiles < 256) return true;
+  const int64_t filled = 100 * rows / (128 * tiles);  // percent of the tiles' rows
+  return filled < (p.P <= 1280 ? 48 : 60);
 }
 // The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
-// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4; 256 rows, 16384 keys, d = 128 in
-// two of 128: 50, two and a half times that in tiles of 32).  Its runs fill half of the chip's places; a prefix that is only
+// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's places; a prefix that is only
 // read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256
 // workgroups 23.1 / 23.0 / 23.8 / 25.6 / 25.9; 96 suffixes, 4001 keys 23.4 / 23.8 / 23.5 / 16.7 / 16.1; 256 rows, 16384 keys,
 // 128 / 256 / 384 / 512 58 / 51 / 55 / 63).
