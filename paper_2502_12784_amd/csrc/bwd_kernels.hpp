@@ -663,7 +663,10 @@ static __device__ __forceinline__ void bwd_dq(
       kv_end = lim < Nk ? lim : Nk;
     }
     if constexpr (Keys::PREFIX) np_part = np + (kv_end + C::BN - 1) / C::BN;
-    const int nt = Keys::PREFIX ? np_part + (keys.P % C::BN != 0) : (kv_end + C::BN - 1) / C::BN;
+    const int n_all = Keys::PREFIX ? np_part + (keys.P % C::BN != 0) : (kv_end + C::BN - 1) / C::BN;
+    // this workgroup's tiles: all of them, or one of `parts` runs
+    const int j0 = Keys::PREFIX ? (int)((int64_t)n_all * keys.part / keys.parts) : 0;
+    const int nt = Keys::PREFIX ? (int)((int64_t)n_all * (keys.part + 1) / keys.parts) : n_all;
 
     LaneOffsets off(lane);  // read offsets of the current buffer
 
@@ -673,7 +676,7 @@ static __device__ __forceinline__ void bwd_dq(
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[dt][r] = 0.f;
 
-    fetch_tile(0, 0);
+    fetch_tile(j0, 0);
     // the tile is requested before the wait for O and dO that forming D takes, not behind it (the scheduler's
     // choice; us, causal 256 heads x 512, d = 128 54.5 -> 48.8, d = 64 31.4 -> 27.9)
     sched_fence();
@@ -690,7 +693,7 @@ static __device__ __forceinline__ void bwd_dq(
       Dq = half_pair_sum(Dq) * (DROP ? dr.keep_prob : 1.0f);
       lse2 *= 1.4426950408889634f;
       if (Keys::PREFIX && lse2 == -INFINITY) lse2 = INFINITY;  // a row without keys: P = exp2(s - inf) = 0
-      if (g == 0 && qrow < q_end) {
+      if (g == 0 && qrow < q_end && (!Keys::PREFIX || keys.part == 0)) {
         Dws[stat] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
         LSE2ws[stat] = lse2;
       }
@@ -717,7 +720,7 @@ static __device__ __forceinline__ void bwd_dq(
     // crosses, and without any mask arithmetic for all the others.
     auto iteration = [&](const int j, auto masked_tag) {
       constexpr bool MASKED = decltype(masked_tag)::value;
-      const int buf = j & 1;
+      const int buf = (j - j0) & 1;
       if (j + 1 < nt) fetch_tile(j + 1, buf ^ 1);  // everybody left that buffer before the last barrier
       // with a prefix: first key of the tile in its part, and whether the part is the prefix
       const bool of_prefix = Keys::PREFIX && (j < np || j >= np_part);
@@ -873,7 +876,7 @@ static __device__ __forceinline__ void bwd_dq(
       n_plain = (q0 + 1) / C::BN;
     }
     if (n_plain > nt) n_plain = nt;
-    int j = 0;
+    int j = j0;
     for (; j < n_plain; ++j) iteration(j, std::false_type{});
     for (; j < nt; ++j) iteration(j, std::true_type{});
     if constexpr (Keys::PREFIX) {
@@ -883,6 +886,16 @@ static __device__ __forceinline__ void bwd_dq(
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) dq[dt][r] = qrow < q_end ? dq[dt][r] : 0.f;  // rows not in use: zeros
+      if (keys.sums) {  // one run's part, as the accumulators hold it (PrefixTile)
+#pragma unroll
+        for (int q = 0; q < D / 8; ++q) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = dq[q / 4][4 * (q % 4) + e];
+          *reinterpret_cast<f32x4*>(keys.sums + (wave * (D / 8) + q) * 256 + lane * 4) = x;
+        }
+        return;
+      }
       store_transposed_to<T, D, C::OSTR>(dq, mul, ob, lane, [&](int row) -> T* {
         return q0 + row < Nq ? dQ + keys.offset(mdq, q0 + row) : nullptr;
       }, dh);

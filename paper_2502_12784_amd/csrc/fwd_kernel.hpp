@@ -62,7 +62,7 @@ template <int D, int NW = 4, bool PAIR = false> struct FwdCfg {
 // The keys of a forward's query tile.  One sequence: rows 0 ... Nk-1 of K and V.
 struct OneSequence {
   static constexpr bool PREFIX = false, PACKED = false;
-  static constexpr int head = 0, item = 0, per = 1, P = 0, rows = 0, ahead = 0, seen = 0;  // not used
+  static constexpr int head = 0, item = 0, per = 1, P = 0, rows = 0, ahead = 0, seen = 0, part = 0, parts = 1;  // not used
   static constexpr uint32_t kp_row_bytes = 0, vp_row_bytes = 0;
   template <typename T>
   __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap& m, int head, int H) const {
@@ -87,6 +87,9 @@ template <typename T> struct PrefixAndSuffix {
   int P;                  // its keys
   int rows;               // packed rows in use, 1 at least; those behind, up to Nq, give zeros and an LSE of -inf
   int ahead;              // query i sees suffix keys j <= i + ahead: causal, or a number that hides none
+  // dQ only: the tile's keys in `parts` runs, of which this is the one; where its sums go then, or nullptr
+  int part = 0, parts = 1;
+  float* sums = nullptr;
   __device__ __forceinline__ const T* head_rows(const T* X, const TensorMap&, int, int) const { return X; }
   // where packed row r is in a tensor, and in LSE
   __device__ __forceinline__ size_t offset(const TensorMap& m, int r) const {

@@ -191,9 +191,23 @@ size_t part_floats(const PrefixProblem& p, int parts, int outer, int n) {
 }
 size_t prefix_part_floats(const PrefixProblem& p, const PrefixShares& x) { return part_floats(p, x.parts, p.G, p.P); }
 size_t suffix_part_floats(const PrefixProblem& p, const PrefixShares& x) { return part_floats(p, x.s_parts, p.B, p.S); }
+// Workgroups that share the keys of a tile of rows in dQ: as many as give every place (two to a CU) one, with eight tiles of
+// keys to each at least, sixteen at most.  (Steps, us, one -> so: 1 head x 192 queries behind 8192 keys, d = 128, 223 -> 44;
+// 2 sequences x 32 heads over 8 x 128 behind 8192, d = 128, 363 -> 246; 5 x 1 x 23 behind 4672, d = 64, 76 -> 33.)
+int64_t dq_tiles(const PrefixProblem& p) { return (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128); }
+int query_parts(const PrefixProblem& p) {
+  const int64_t tiles = ((int64_t)p.P + p.S + 63) / 64 * (p.dh > 96 ? 2 : 1);
+  int64_t parts = 512 / dq_tiles(p);
+  if (parts > tiles / 8) parts = tiles / 8;
+  return parts > 16 ? 16 : parts < 1 ? 1 : (int)parts;
+}
+size_t query_part_floats(const PrefixProblem& p) {
+  const int parts = query_parts(p);
+  return parts > 1 ? (size_t)parts * (size_t)dq_tiles(p) * 128 * (p.dh <= 64 ? 64 : p.dh <= 96 ? 96 : 128) : 0;
+}
 size_t prefix_bwd_workspace(const PrefixProblem& p) {
   const PrefixShares x = prefix_shares(p);
-  return prefix_stats_bytes(p) + sizeof(float) * (prefix_part_floats(p, x) + suffix_part_floats(p, x));
+  return prefix_stats_bytes(p) + sizeof(float) * (prefix_part_floats(p, x) + suffix_part_floats(p, x) + query_part_floats(p));
 }
 
 // Whether dQ and dK/dV run in one grid: where dQ's tiles alone leave CUs idle.  In one grid dQ, which has two workgroups to a
@@ -204,15 +218,14 @@ size_t prefix_bwd_workspace(const PrefixProblem& p) {
 //   d = 128:  4 x 16 over 4 x 256 behind 512 (128) 88.4 -> 83.9                          8 x 16 x 256 behind 1024 (256) 131.0 -> 136.2
 //             8 x 16 over 4 x 512 behind 2048 (512) 311.7 -> 354.9
 bool prefix_merged(const PrefixProblem& p) {
-  const int64_t dq = (int64_t)p.B * p.Hkv * (((int64_t)p.Nq * (p.H / p.Hkv) + 127) / 128);
-  return dq <= (p.dh <= 64 ? 512 : p.dh <= 96 ? 288 : 192);
+  return dq_tiles(p) <= (p.dh <= 64 ? 512 : p.dh <= 96 ? 288 : 192);
 }
 
 template <typename T, int D>
 int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, float scale, bool merged, hipStream_t st) {
   using Q = BwdQCfg<D, true, false>;
   using C = BwdKvPipeCfg<D>;
-  const int nqt = (p.Nq * (p.H / p.Hkv) + Q::BM - 1) / Q::BM, dq_items = p.B * p.Hkv * nqt;
+  const int nqt = (p.Nq * (p.H / p.Hkv) + Q::BM - 1) / Q::BM, dq_items = p.B * p.Hkv * nqt * gr.q_parts;
   const int p_tiles = (p.P + C::BN - 1) / C::BN, s_tiles = (p.S + C::BN - 1) / C::BN;
   const int first = p.G * p.Hkv * gr.parts * p_tiles, grid = first + p.B * p.Hkv * s_tiles * gr.s_parts;
   if (merged) {
@@ -243,10 +256,11 @@ int launch_prefix_bwd(const PrefixProblem& p, const void* O, PrefixGrads<T> gr, 
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), C::SMEM, st, p, gr, p_tiles, s_tiles, first, scale);
     if (!launch_ok("dK/dV kernel (prefix)")) return SPARK_ERR_LAUNCH;
   }
-  if (gr.parts == 1 && gr.s_parts == 1) return SPARK_OK;
+  if (gr.parts == 1 && gr.s_parts == 1 && gr.q_parts == 1) return SPARK_OK;
   const int p_blocks = gr.parts > 1 ? p.G * p.Hkv * p_tiles * 4 : 0, s_blocks = gr.s_parts > 1 ? p.B * p.Hkv * s_tiles * 4 : 0;
-  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)(p_blocks + s_blocks)), dim3(1024), 0, st, p, gr, p_blocks,
-                     p_tiles, s_tiles, scale);
+  const int q_blocks = gr.q_parts > 1 ? p.B * p.Hkv * nqt * 4 : 0;
+  hipLaunchKernelGGL((mha_prefix_sum_kernel<T, D>), dim3((unsigned)(p_blocks + s_blocks + q_blocks)), dim3(1024), 0, st, p, gr,
+                     p_blocks, s_blocks, p_tiles, s_tiles, nqt, scale);
   return launch_ok("sum of the parts (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
@@ -277,6 +291,8 @@ int dispatch_prefix_bwd(const PrefixProblem& p, const void* O, const PrefixGradA
   gr.s_parts = x.s_parts;
   gr.s_run = x.s_run;
   gr.partial_s = gr.partial + prefix_part_floats(p, x);
+  gr.q_parts = query_parts(p);
+  gr.partial_q = gr.partial_s + suffix_part_floats(p, x);
   const bool merged = prefix_merged(p);
   if (p.dh <= 64) return launch_prefix_bwd<T, 64>(p, O, gr, scale, merged, st);
   if (p.dh <= 96) return launch_prefix_bwd<T, 96>(p, O, gr, scale, merged, st);

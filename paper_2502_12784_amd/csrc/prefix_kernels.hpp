@@ -130,6 +130,8 @@ template <typename T> struct PrefixGrads {
   float* partial_s;     // if s_parts > 1: [s_parts][B * Hkv][tiles of S], of the suffix tiles that several workgroups share
   int parts;            // workgroups that share a prefix tile's stages evenly
   int s_parts, s_run;   // a suffix tile's stages in runs of s_run; s_parts is the most runs a tile can have
+  float* partial_q;     // if q_parts > 1: [q_parts][B * Hkv][tiles of packed rows] tiles of dQ / scale, as PrefixTile but one tensor
+  int q_parts;          // workgroups that share the keys of a tile of rows
 };
 
 // A part of a tile's dK / scale and dV in fp32, as the accumulators hold them: [wave][eight columns of dK, then of dV][lane][4],
@@ -137,6 +139,7 @@ template <typename T> struct PrefixGrads {
 // instead, whose stores are pieces of 32 bytes: dK/dV of the 16 sequences above 207.3 us, so 205.4.)
 template <int D> struct PrefixTile {
   static constexpr int EIGHTS = 2 * D / 8, WAVE = EIGHTS * 256, FLOATS = 4 * WAVE;
+  static constexpr int Q_WAVE = WAVE / 2, Q_FLOATS = FLOATS / 2;  // of dQ
 };
 
 // Of a suffix tile from key k0 on: the first block of 64 queries that sees it, and how many blocks from there on; per head.
@@ -150,19 +153,23 @@ struct SuffixBlocks {
   }
 };
 
-// The workgroup's part of dQ: tile `logical` of all sequences' and heads' tiles.  STATS: D and LSE * log2(e) are there already.
+// The workgroup's part of dQ: `logical` counts the runs of keys of all sequences' and heads' tiles of rows.  A long prefix
+// behind few rows is a long chain in few workgroups otherwise.  STATS: D and LSE * log2(e) are there already.
 template <typename T, int D, bool STATS>
 static __device__ __forceinline__ void prefix_dq(const PrefixProblem& p, const T* __restrict__ O, const PrefixGrads<T>& gr, int nqt,
                                                  float scale, int logical) {
+  const int part = logical % gr.q_parts;
+  logical /= gr.q_parts;
   const int flat = logical / nqt, item = logical - flat * nqt;
   const PrefixHead x(p, flat);
-  const PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
+  PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
   const int h0 = x.hk * keys.per, all = p.Nq * keys.per;
   T* const dQ = gr.dQ + (size_t)x.b * (size_t)gr.mdq.batch + (size_t)h0 * (size_t)gr.mdq.head;
   const size_t stats = ((size_t)x.b * p.H + h0) * (size_t)p.Nq;
   constexpr int BM = BwdQCfg<D, true, false>::BM;
   const int row0 = (nqt - 1 - item) * BM, row1 = row0 + BM < all ? row0 + BM : all;
   if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
+    if (part) return;
     zero_rows(dQ, gr.mdq, keys, row0, row1, p.dh);
     if (!STATS) {
       for (int r = row0 + threadIdx.x; r < row1; r += 256) {
@@ -171,6 +178,12 @@ static __device__ __forceinline__ void prefix_dq(const PrefixProblem& p, const T
       }
     }
     return;
+  }
+  if (gr.q_parts > 1) {
+    keys.part = part;
+    keys.parts = gr.q_parts;
+    const size_t tiles = (size_t)p.B * (size_t)p.Hkv * (size_t)nqt, tile = ((size_t)x.b * p.Hkv + x.hk) * (size_t)nqt + (nqt - 1 - item);
+    keys.sums = gr.partial_q + ((size_t)part * tiles + tile) * PrefixTile<D>::Q_FLOATS;
   }
   bwd_dq<T, D, true, false, STATS, IN_ORDER>(
       head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk), head_of<T>(p.Vs, p.mvs, x.b, x.hk),
@@ -436,7 +449,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_dkdv_kernel(P
 template <typename T, int D>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void mha_prefix_bwd_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_tiles,
                                                                               int s_tiles, int first, int nqt, float scale) {
-  const int dq_items = p.B * p.Hkv * nqt, block = blockIdx.x;
+  const int dq_items = p.B * p.Hkv * nqt * gr.q_parts, block = blockIdx.x;
   if (block >= first && block < first + dq_items)
     prefix_dq<T, D, true>(p, nullptr, gr, nqt, scale, xcd_contiguous(block - first, dq_items));
   else
@@ -468,16 +481,64 @@ __global__ __launch_bounds__(256) void mha_prefix_stats_kernel(PrefixProblem p, 
   }
 }
 
-// dK and dV of the tiles that several workgroups share, from the parts, added in their order: a workgroup per 32 keys, first of
-// the prefixes (p_blocks workgroups), then of the suffixes.
-template <typename T, int D>
-__global__ __launch_bounds__(1024) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_blocks, int p_tiles,
-                                                             int s_tiles, float scale) {
+// Sum of the parts of 32 rows of a tile, in their order, times `mul_first` in the first `first` eights of columns; rounded into
+// `rows`.  1024 threads; four parts are requested together.
+template <typename T, int EIGHTS>
+static __device__ __forceinline__ void sum_parts(const float* x, size_t step, int parts, int first, float mul_first,
+                                                 T (&rows)[32][8 * EIGHTS + 8]) {
   using v4 = typename Frag<T>::v4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  x += lane * 4;
+#pragma unroll
+  for (int q = wave; q < EIGHTS; q += 16) {
+    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < parts; i += 4) {
+      f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4*>(x + (i + u < parts ? i + u : i) * step + q * 256);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i + u < parts) a += v[u];
+      }
+    }
+    const float mul = q < first ? mul_first : 1.0f;
+    v4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (T)(a[e] * mul);
+    *reinterpret_cast<v4*>(&rows[lane & 31][8 * q + 4 * (lane >> 5)]) = r;
+  }
+  __syncthreads();
+}
+
+// Gradients of the tiles that several workgroups share: a workgroup per 32 rows, first of the prefixes' keys (p_blocks
+// workgroups), then of the suffixes' (s_blocks), then of the queries.
+template <typename T, int D>
+__global__ __launch_bounds__(1024) void mha_prefix_sum_kernel(PrefixProblem p, PrefixGrads<T> gr, int p_blocks, int s_blocks,
+                                                              int p_tiles, int s_tiles, int nqt, float scale) {
   using Tile = PrefixTile<D>;
+  const int block = blockIdx.x;
+  if (block >= p_blocks + s_blocks) {
+    __shared__ __align__(16) T rows[32][D + 8];
+    const int id = block - p_blocks - s_blocks, quarter = id & 3, at = id >> 2, owner = at / nqt, tile = at - owner * nqt,
+              b = owner / p.Hkv, hk = owner - b * p.Hkv, per = p.H / p.Hkv, row0 = tile * 128 + quarter * 32;
+    // what no workgroup took on is zero already
+    const int q = length_of(p.q_lens, b, p.Nq), S = length_of(p.s_lens, b, p.S), P = length_of(p.prefix_lens, b / (p.B / p.G), p.P);
+    const int all = p.Nq * per, end = tile * 128 + 128 < all ? tile * 128 + 128 : all;
+    if (tile * 128 >= q * per || (P == 0 && (S == 0 || (end - 1) / per + (p.causal ? S - q : ALL_AHEAD) < 0))) return;
+    const size_t step = (size_t)p.B * (size_t)p.Hkv * (size_t)nqt * Tile::Q_FLOATS;
+    sum_parts<T, D / 8>(gr.partial_q + (size_t)at * Tile::Q_FLOATS + quarter * Tile::Q_WAVE, step, gr.q_parts, D / 8, scale, rows);
+    T* const dQ = gr.dQ + (size_t)b * (size_t)gr.mdq.batch + (size_t)(hk * per) * (size_t)gr.mdq.head;
+    for (int i = threadIdx.x; i < 32 * (D / 8); i += 1024) {
+      const int r = row0 + i / (D / 8), col = i % (D / 8) * 8, query = r / per;
+      if (r >= all || col >= p.dh) continue;
+      *reinterpret_cast<u32x4*>(dQ + (size_t)query * (size_t)gr.mdq.row + (size_t)(r - query * per) * (size_t)gr.mdq.head + col) =
+          *reinterpret_cast<const u32x4*>(&rows[r - row0][col]);
+    }
+    return;
+  }
   __shared__ __align__(16) T rows[32][2 * D + 8];
-  const bool of_prefix = (int)blockIdx.x < p_blocks;
-  const int id = of_prefix ? blockIdx.x : (int)blockIdx.x - p_blocks, quarter = id & 3, at = id >> 2;
+  const bool of_prefix = block < p_blocks;
+  const int id = of_prefix ? block : block - p_blocks, quarter = id & 3, at = id >> 2;
   const int tiles = of_prefix ? p_tiles : s_tiles, owner = at / tiles, tile = at - owner * tiles, outer = owner / p.Hkv,
             hk = owner - outer * p.Hkv, key0 = tile * 128 + quarter * 32;
   int parts = gr.parts, keys;
@@ -492,28 +553,9 @@ __global__ __launch_bounds__(1024) void mha_prefix_sum_kernel(PrefixProblem p, P
     parts = (stages + gr.s_run - 1) / gr.s_run;
   }
   if (key0 >= keys) return;  // zeros already
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float* x = (of_prefix ? gr.partial : gr.partial_s) + (size_t)at * Tile::FLOATS + quarter * Tile::WAVE + lane * 4;
   const size_t step = (size_t)(of_prefix ? p.G : p.B) * (size_t)p.Hkv * (size_t)tiles * Tile::FLOATS;
-#pragma unroll
-  for (int q = wave; q < Tile::EIGHTS; q += 16) {
-    f32x4 a = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < parts; i += 4) {  // four requested together
-      f32x4 v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4*>(x + (i + u < parts ? i + u : i) * step + q * 256);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (i + u < parts) a += v[u];
-      }
-    }
-    const float mul = q < Tile::EIGHTS / 2 ? scale : 1.0f;
-    v4 r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (T)(a[e] * mul);
-    *reinterpret_cast<v4*>(&rows[lane & 31][8 * q + 4 * (lane >> 5)]) = r;
-  }
-  __syncthreads();
+  sum_parts<T, Tile::EIGHTS>((of_prefix ? gr.partial : gr.partial_s) + (size_t)at * Tile::FLOATS + quarter * Tile::WAVE, step, parts,
+                             D / 8, scale, rows);
   T* const dK = of_prefix ? gr.dKp : gr.dKs;
   T* const dV = of_prefix ? gr.dVp : gr.dVs;
   const TensorMap &mk = of_prefix ? gr.mdkp : gr.mdks, &mv = of_prefix ? gr.mdvp : gr.mdvs;
