@@ -371,7 +371,7 @@ PyObject* host_qk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Here h;
   QkCall c;
-  if (n != 11 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (n != 11 || !get_device || modes_active() || !plain(a[0], 4)) Py_RETURN_NONE;
   if (!here(&h)) return nullptr;
   Arguments args(h.device);
   if (!qk_call(args, a, a[6], a[7], a[8], &c)) Py_RETURN_NONE;
@@ -397,7 +397,7 @@ PyObject* host_qk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Here h;
   QkCall c;
-  if (n != 15 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (n != 15 || !get_device || modes_active() || !plain(a[0], 4)) Py_RETURN_NONE;
   if (!here(&h)) return nullptr;
   Arguments args(h.device);
   if (!qk_call(args, a, a[8], a[9], a[10], &c)) Py_RETURN_NONE;
@@ -473,7 +473,7 @@ PyObject* host_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Here h;
   PrefixCall c;
-  if (n != 12 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (n != 12 || !get_device || modes_active() || !plain(a[0], 4)) Py_RETURN_NONE;
   if (!here(&h)) return nullptr;
   Arguments args(h.device);
   if (!prefix_call(args, a, a + 5, &c)) Py_RETURN_NONE;
@@ -505,7 +505,7 @@ PyObject* host_prefix_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   Here h;
   PrefixCall c;
-  if (n != 18 || !get_device || modes_active()) Py_RETURN_NONE;
+  if (n != 18 || !get_device || modes_active() || !plain(a[0], 4)) Py_RETURN_NONE;
   if (!here(&h)) return nullptr;
   Arguments args(h.device);
   if (!prefix_call(args, a, a + 8, &c)) Py_RETURN_NONE;
