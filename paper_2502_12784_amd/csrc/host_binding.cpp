@@ -15,7 +15,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/ExpandUtils.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <ATen/record_function.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -121,6 +123,20 @@ class Allocator {
     for (int i = 3; i >= 0; stride *= t.size(i--))
       if (t.stride(i) != stride || t.size(i) < 1) return at::empty_like(t);
     return contiguous(t.sizes(), t.scalar_type());
+  }
+
+  // the same for views, whose layouts empty_like works out in Python-visible steps: its order of the dimensions, without gaps
+  // (slices of a packed projection: norm and rotation of one token in eight sequences 6.7 -> 5.9 us a call)
+  at::Tensor like(const at::Tensor& t) const {
+    if (!direct_ || t.has_names()) return at::empty_like(t);
+    const at::IntArrayRef sizes = t.sizes();
+    const auto dense = [&](at::IntArrayRef strides) {
+      return at::_ops::empty_strided::redispatch(c10::DispatchKeySet(c10::DispatchKey::CUDA), c10::fromIntArrayRefSlow(sizes),
+                                                 c10::fromIntArrayRefSlow(strides), t.scalar_type(), c10::Layout::Strided,
+                                                 like_.device(), std::nullopt);
+    };
+    if (t.is_non_overlapping_and_dense()) return dense(t.strides());
+    return dense(at::infer_dense_strides(sizes, t.strides()));
   }
 
  private:
@@ -378,7 +394,7 @@ PyObject* host_qk_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor *Qr = args.given(a[9], c.st, c.B, c.H, c.N, c.d), *Kr = args.given(a[10], c.st, c.B, c.Hkv, c.N, c.d);
   if (!args.ok) Py_RETURN_NONE;
   const Allocator fresh(*c.Q);
-  const at::Tensor q = Qr ? *Qr : fresh.same(*c.Q), k = Kr ? *Kr : fresh.same(*c.K);
+  const at::Tensor q = Qr ? *Qr : fresh.like(*c.Q), k = Kr ? *Kr : fresh.like(*c.K);
   void *qp = q.data_ptr(), *kp = k.data_ptr();
   const void *Qp = c.Q->data_ptr(), *Kp = c.K->data_ptr();
   const spark_strides_t sQ = of(*c.Q), sK = of(*c.K), sq = of(q), sk = of(k);
@@ -407,7 +423,7 @@ PyObject* host_qk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (int i = 0; i < 2; ++i) dwg[i] = a[13 + i] == Py_None ? nullptr : args.dense(a[13 + i], at::kFloat, {c.d});
   if (!args.ok) Py_RETURN_NONE;
   const Allocator fresh(*c.Q);
-  const at::Tensor dQ = dQg ? *dQg : fresh.same(*c.Q), dK = dKg ? *dKg : fresh.same(*c.K);
+  const at::Tensor dQ = dQg ? *dQg : fresh.like(*c.Q), dK = dKg ? *dKg : fresh.like(*c.K);
   const at::Tensor dwq = dwg[0] ? *dwg[0] : fresh.contiguous({c.d}, at::kFloat),
                    dwk = dwg[1] ? *dwg[1] : fresh.contiguous({c.d}, at::kFloat);
   const size_t need = spark_qk_norm_rope_bwd_workspace_bytes(c.B, c.N, c.H, c.Hkv, c.d, c.rd, c.code);
@@ -481,7 +497,7 @@ PyObject* host_prefix_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor* Lg = a[11] == Py_None ? nullptr : args.dense(a[11], at::kFloat, {c.B, c.H, c.Nq});
   if (!args.ok) Py_RETURN_NONE;
   const Allocator fresh(*c.x[0]);
-  const at::Tensor O = Og ? *Og : fresh.same(*c.x[0]), L = Lg ? *Lg : fresh.contiguous({c.B, c.H, c.Nq}, at::kFloat);
+  const at::Tensor O = Og ? *Og : fresh.like(*c.x[0]), L = Lg ? *Lg : fresh.contiguous({c.B, c.H, c.Nq}, at::kFloat);
   const size_t need = spark_mha_prefix_fwd_workspace_bytes(c.G, c.B, c.H, c.Hkv, c.Nq, c.P, c.S, c.d, c.code);
   at::Tensor ws;
   if (need) ws = fresh.contiguous({(int64_t)need}, at::kByte);
@@ -520,7 +536,7 @@ PyObject* host_prefix_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   void* gp[5];
   spark_strides_t gs[5];
   for (int i = 0; i < 5; ++i) {
-    g[i] = given[i] ? *given[i] : fresh.same(*c.x[i]);
+    g[i] = given[i] ? *given[i] : fresh.like(*c.x[i]);
     gp[i] = g[i].data_ptr();
     gs[i] = of(g[i]);
   }

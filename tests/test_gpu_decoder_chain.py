@@ -154,3 +154,20 @@ def test_two_threads_on_streams_of_their_own():
     for t in threads:
         t.join()
     assert not bad
+
+
+def test_allocated_outputs_have_the_layouts_of_empty_like():
+    from paper_2502_12784_amd import spark_mha_prefix_bwd, spark_mha_prefix_fwd, spark_qk_norm_rope_fwd
+    x = torch.randn(3, 20, 8, 64, device="cuda").to(F16).permute(0, 2, 1, 3)  # [B, heads, N, d], heads inside
+    w = torch.ones(64, device="cuda")
+    cos, sin = du.tables(20, 64)
+    views = [(x[:, :4], x[:, 4:6], x[:, 6:]), (x[:, :4].contiguous(), x[:, 4:6], x[:1, 6:].expand(3, -1, -1, -1)),
+             (x[:, :4, :1], x[:, 4:6, :1], x[:, 6:, :1]), (x[:1, :1], x[:1, 4:5], x[:1, 6:7])]
+    for Q, K, V in views:
+        q, k = spark_qk_norm_rope_fwd(Q, K, w, w, cos, sin)
+        Kp = torch.randn(1, K.shape[1], 30, 64, device="cuda").to(F16)
+        O, LSE = spark_mha_prefix_fwd(Q, Kp, Kp, K, V, 0.125)
+        grads = spark_mha_prefix_bwd(Q, Kp, Kp, K, V, O, LSE, O, 0.125)
+        for got, like in zip((q, k, O, *grads), (Q, K, Q, Q, Kp, Kp, K, V)):
+            want = torch.empty_like(like)
+            assert got.shape == want.shape and got.stride() == want.stride() and got.dtype == want.dtype
