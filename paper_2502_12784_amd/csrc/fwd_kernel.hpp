@@ -78,7 +78,7 @@ struct OneSequence {
 // over 4, forward 86.1 -> FWDUS, dQ 118.5 -> DQUS).
 template <typename T> struct PrefixAndSuffix {
   static constexpr bool PREFIX = true, PACKED = false;
-  static constexpr int head = 0;
+  static constexpr int head = 0, seen = 0;  // not used
   int item;               // the workgroup's tile of rows
   int per, queries;       // heads, and queries of each (the stride of LSE's heads)
   const T *Kp, *Vp;       // of this head

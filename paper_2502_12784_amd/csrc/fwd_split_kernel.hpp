@@ -72,11 +72,11 @@ static __device__ __forceinline__ void fwd_split_tiles(
   const int items = paired ? causal_items<CAUSAL>(nqt) : nqt;
   const int flat = xcd_contiguous(blockIdx.x, gridDim.x);
   const int logical = PART ? flat / parts : flat, part = PART ? flat - logical * parts : 0;
-  const int head = Keys::PACKED ? 0 : logical / items;
-  const int item = Keys::PACKED ? 0 : logical - head * items;
+  const int head = Keys::PACKED || Keys::PREFIX ? 0 : logical / items;
+  const int item = Keys::PREFIX ? keys.item : Keys::PACKED ? 0 : logical - head * items;
 
-  const BufView kview(keys.head_rows(K, mk, head, H), head_span_bytes(mk, Nk, dh));
-  const BufView vview(keys.head_rows(V, mv, head, H), head_span_bytes(mv, Nk, dh));
+  const BufView kview(keys.head_rows(K, mk, head, H), Keys::PREFIX && Nk == 0 ? 0u : head_span_bytes(mk, Nk, dh));
+  const BufView vview(keys.head_rows(V, mv, head, H), Keys::PREFIX && Nk == 0 ? 0u : head_span_bytes(mv, Nk, dh));
   const uint32_t k_row_bytes = (uint32_t)mk.row * 2, v_row_bytes = (uint32_t)mv.row * 2;
   const WaveDma<D> kdma(lane, k_row_bytes, dh), vdma(lane, v_row_bytes, dh);
   const SwzLane<D> off(lane);
@@ -91,12 +91,20 @@ static __device__ __forceinline__ void fwd_split_tiles(
     const T* qp;
     if constexpr (Keys::PACKED)
       qp = keys.q;
+    else if constexpr (Keys::PREFIX)
+      qp = Q + keys.offset(mq, qrow < keys.rows ? qrow : keys.rows - 1);
     else
       qp = Q + head_base(mq, head, H) + (size_t)(qrow < Nq ? qrow : Nq - 1) * (size_t)mq.row;
 
     int kv_end = Nk;
     if (CAUSAL && q0 + C::BM < Nk) kv_end = q0 + C::BM;
-    int nt = (kv_end + C::BN - 1) / C::BN;
+    if constexpr (Keys::PREFIX) {
+      const int lim = (q0 + C::BM - 1) / keys.per + 1 + keys.ahead;
+      kv_end = lim < 0 ? 0 : lim < Nk ? lim : Nk;
+    }
+    // with a prefix, tiles [0, np) are its tiles; the suffix's follow
+    const int np = Keys::PREFIX ? (keys.P + C::BN - 1) / C::BN : 0;
+    int nt = np + (kv_end + C::BN - 1) / C::BN;
     int j0 = 0;  // this workgroup's tiles are [j0, nt)
     if (PART && !Keys::PACKED) {
       const int per = (nt + parts - 1) / parts;
@@ -107,6 +115,10 @@ static __device__ __forceinline__ void fwd_split_tiles(
     int n_plain = Nk / C::BN;
     if (CAUSAL && (q0 + 1) / C::BN < n_plain) n_plain = (q0 + 1) / C::BN;
     if constexpr (Keys::PACKED) n_plain = keys.seen_by_all / C::BN;
+    if constexpr (Keys::PREFIX) {  // of the suffix
+      const int first = q0 / keys.per + keys.ahead + 1;  // keys that the tile's first row sees
+      if (first / C::BN < n_plain) n_plain = first < 0 ? 0 : first / C::BN;
+    }
 
     v8 qf[KS];
     load_row_frags(qf, qp, g, dh);
@@ -127,8 +139,26 @@ static __device__ __forceinline__ void fwd_split_tiles(
     float m_run = -1e30f;  // finite, so that a masked score (-inf) minus the reference is not NaN
     float l_run = 0.f;
 
-    auto fetch_k = [&](int j) { kdma.template tile<C::BN>(kview, j * C::BN, kb, k_row_bytes); };
-    auto fetch_v = [&](int j) { vdma.template tile<C::BN>(vview, j * C::BN, vb, v_row_bytes); };
+    auto fetch_k = [&](int j) {
+      if constexpr (Keys::PREFIX) {
+        if (j < np) {
+          WaveDma<D>(lane, keys.kp_row_bytes, dh).template tile<C::BN>(BufView(keys.Kp, keys.kp_bytes), j * C::BN, kb,
+                                                                      keys.kp_row_bytes);
+          return;
+        }
+      }
+      kdma.template tile<C::BN>(kview, (j - np) * C::BN, kb, k_row_bytes);
+    };
+    auto fetch_v = [&](int j) {
+      if constexpr (Keys::PREFIX) {
+        if (j < np) {
+          WaveDma<D>(lane, keys.vp_row_bytes, dh).template tile<C::BN>(BufView(keys.Vp, keys.vp_bytes), j * C::BN, vb,
+                                                                      keys.vp_row_bytes);
+          return;
+        }
+      }
+      vdma.template tile<C::BN>(vview, (j - np) * C::BN, vb, v_row_bytes);
+    };
     if (j0 + wave < nt) {
       fetch_k(j0 + wave);
       fetch_v(j0 + wave);
@@ -136,7 +166,9 @@ static __device__ __forceinline__ void fwd_split_tiles(
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));  // Q is awaited here, not in the loop
 
-    const int last_key = (Keys::PACKED ? keys.seen - 1 : CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;  // as in mha_fwd_kernel
+    const int query = Keys::PREFIX ? qrow / keys.per : qrow;
+    const int last_key = (Keys::PREFIX ? (query < Nk - keys.ahead ? query + keys.ahead : Nk - 1)
+                          : Keys::PACKED ? keys.seen - 1 : CAUSAL && qrow < Nk ? qrow : Nk - 1) - 4 * g;  // as in mha_fwd_kernel
     // One tile; next: this wave has another one.  On entry at most NLOAD loads of K and, behind them,
     // NLOAD of V are outstanding.
     auto tile = [&](const int j, auto masked_tag, const bool next) {
@@ -168,7 +200,8 @@ static __device__ __forceinline__ void fwd_split_tiles(
         for (int r = 0; r < 16; ++r) {
           t[h * 16 + r] = s[h][r];
           if (MASKED) {
-            if (h * 32 + 8 * (r / 4) + (r % 4) > last_key - k0) t[h * 16 + r] = -INFINITY;
+            if (h * 32 + 8 * (r / 4) + (r % 4) > (Keys::PREFIX && j < np ? keys.P - 1 - 4 * g : last_key + np * C::BN) - k0)
+              t[h * 16 + r] = -INFINITY;
           }
         }
       };
@@ -234,6 +267,14 @@ static __device__ __forceinline__ void fwd_split_tiles(
       }
     };
     int j = j0 + wave;
+    if constexpr (Keys::PREFIX) {
+      for (; j < nt; j += C::NW) {
+        if (j < np ? j < keys.P / C::BN : j - np < n_plain)
+          tile(j, std::false_type{}, j + C::NW < nt);
+        else
+          tile(j, std::true_type{}, j + C::NW < nt);
+      }
+    }
     if (n_plain > nt) n_plain = nt;
     for (; j < n_plain; j += C::NW) tile(j, std::false_type{}, j + C::NW < nt);
     for (; j < nt; j += C::NW) tile(j, std::true_type{}, j + C::NW < nt);
@@ -252,6 +293,7 @@ static __device__ __forceinline__ void fwd_split_tiles(
     float l_all = 0.f;
     for (int w = 0; w < used; ++w)
       l_all += stat[(C::NW + w) * C::BM + c32] * __builtin_amdgcn_exp2f(stat[w * C::BM + c32] - m_all);
+    const bool empty = Keys::PREFIX && (l_all == 0.f || qrow >= keys.rows);  // no key, or not a row in use: zeros
     const float mul = __builtin_amdgcn_exp2f(m_run - m_all) * (PART ? 1.0f : (DROP ? dr.rescale : 1.0f) / l_all);
     const size_t prow = ((size_t)head * Nq + qrow) * (size_t)(PART ? parts : 1) + part;  // row of the partial result
     if (wave < used) {
@@ -280,7 +322,7 @@ static __device__ __forceinline__ void fwd_split_tiles(
       }
       v4 pk;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) pk[e] = (T)sum[e];
+      for (int e = 0; e < 4; ++e) pk[e] = (T)(empty ? 0.f : sum[e]);
       lds_write(smem + C::STG0, c32 * C::OSTR + (8 * q + 4 * g) * 2, pk);
     }
     if constexpr (Keys::PACKED) {
@@ -296,6 +338,15 @@ static __device__ __forceinline__ void fwd_split_tiles(
     __syncthreads();
     constexpr int CPR = D / 8;
     const int row = tid / CPR, cc = tid % CPR;
+    if constexpr (Keys::PREFIX) {
+      for (int r = row; r < C::BM; r += 64 * C::NW / CPR) {
+        if (q0 + r < Nq && cc * 8 < dh)
+          *reinterpret_cast<u32x4*>(O + keys.offset(mo, q0 + r) + cc * 8) = lds_read16<u32x4>(smem, C::STG0 + r * C::OSTR + cc * 16);
+      }
+      if (wave == 0 && g == 0 && qrow < Nq)
+        LSE[keys.stat(qrow)] = empty ? -INFINITY : (m_all + __builtin_amdgcn_logf(l_all)) * 0.6931471805599453f;
+      return;
+    }
     if (row < C::BM && q0 + row < Nq && cc * 8 < dh)
       *reinterpret_cast<u32x4*>(O + head_base(mo, head, H) + (size_t)(q0 + row) * (size_t)mo.row + cc * 8) =
           lds_read16<u32x4>(smem + C::STG0, row * C::OSTR + cc * 16);

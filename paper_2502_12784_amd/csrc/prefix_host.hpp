@@ -57,19 +57,27 @@ bool prefix_wide(const PrefixProblem& p) {
   return (int64_t)p.P + p.S >= 2048 && 7 * wide <= 4 * narrow && (wide >= 512 || narrow >= 896 || (wide <= 256 && narrow > 256));
 }
 
+// Whether 32 packed rows of a sequence go to a workgroup with all their keys (mha_prefix_short_kernel): up to four rounds of its
+// key streams, while the workgroups are resident together or a sequence's rows fit one.  Forward, us, otherwise / so, sequences x
+// heads x queries behind P + S keys:
+//   d = 128:  32 x 16 x 1 behind 64 + 64 9.9 / 9.7, 256 + 64 13.9 / 11.8, 384 + 64 14.0 / 13.2, 640 + 64 14.4 / 16.1
+//             8 x 16 x 16 behind 256 + 64 12.8 / 8.8, 512 + 64 13.8 / 11.0, 1024 + 64 15.5 / 16.3     8 x 16 x 64 behind 128 + 64 9.2 / 8.5
+//             4 x 32 over 8 x 1 behind 128 + 200 9.4 / 8.6, 512 + 200 9.8 / 11.8     64 x 32 over 8 x 1 behind 128 + 100 17.2 / 11.4
+//   d = 64:   2 x 4 x 1 behind 64 + 20 6.3 / 5.6, 512 + 20 8.3 / 8.1, 1024 + 20 8.4 / 10.3     1 x 8 x 100 behind 100 + 100 8.5 / 6.1
+bool prefix_short(const PrefixProblem& p) {
+  const int64_t tiles = ((int64_t)p.Nq * (p.H / p.Hkv) + 31) / 32;
+  return (int64_t)p.P + p.S <= (p.dh <= 64 ? 640 : 512) && (tiles == 1 || p.B * (int64_t)p.Hkv * tiles <= 512);
+}
+
 // Whether rows are packed across sequences and the keys go to several workgroups in runs (prefix_parts.hpp), or every tile of a
-// sequence's rows walks all its keys by itself.  The latter for up to three tiles of keys, where a second kernel costs more than
-// anything saves, and where its tiles fill the chip and are well filled themselves.  Forward, us, d = 128 but where said, packed
-// / by themselves:
-//   32 sequences x 16 heads x 1 behind 64 / 128 / 192 / 256 keys   14.0 / 10.5   13.9 / 11.8   13.9 / 13.3   13.8 / 14.7
-//   2 x 4 x 1, d = 64, behind 64 / 128 / 192 / 256                  7.0 / 6.3   7.2 / 7.0   7.3 / 7.7   7.5 / 8.5
+// sequence's rows walks all its keys by itself: where those tiles fill the chip and are well filled themselves.  Forward, us,
+// d = 128 but where said, packed / by themselves:
 //   rows of a tile in use, half: 32 x 16 x 64 behind 1024 42.5 / 36.7, d = 64 28.4 / 24.9; 64 x 32 over 8 x 16 behind 2048 62.6 / 70.6;
 //   a third: 64 x 16 x 48 behind 2048 82.8 / 125, 32 x 16 x 40 behind 1024 32.4 / 35.4; a quarter: 64 x 16 x 32 behind 2048 57 / 119;
 //   three quarters: 16 x 16 x 96 behind 1024 36.2 / 27.0, 16 x 64 over 16 x 24 behind 2048 47.5 / 40.6
 //   few tiles (n): 2 x 16 x 256 behind 4096 (64) 35 / 73, 4 x 16 x 256 (128) 55 / 74, 8 x 16 x 160 behind 2048 (256) 46.0 / 43.6
 bool prefix_packed(const PrefixProblem& p) {
   const int64_t rows = (int64_t)p.Nq * (p.H / p.Hkv), tiles = (rows + 127) / 128;
-  if (((int64_t)p.P + 63) / 64 + ((int64_t)p.S + 63) / 64 <= 3) return false;
   if (p.B * (int64_t)p.Hkv * tiles < 256) return true;
   const int64_t filled = 100 * rows / (128 * tiles);  // percent of the tiles' rows
   return filled < (p.P <= 1280 ? 48 : 60);
@@ -101,7 +109,7 @@ PrefixParts prefix_runs(const PrefixProblem& p) {
   return s;
 }
 size_t prefix_fwd_workspace(const PrefixProblem& p) {
-  if (!prefix_packed(p)) return 0;
+  if (prefix_short(p) || !prefix_packed(p)) return 0;
   const PrefixParts s = prefix_runs(p);
   return (size_t)p.B * p.H * p.Nq * (size_t)(s.p_parts + s.s_parts) * ((p.dh <= 64 ? 64 : 128) + 4) * sizeof(float);
 }
@@ -132,8 +140,23 @@ int launch_prefix_parts(const PrefixProblem& p, void* O, float* LSE, void* works
   return launch_ok("forward merge kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
+template <typename T, int W>
+int launch_prefix_short(const PrefixProblem& p, void* O, float* LSE, float scale, hipStream_t st) {
+  using C = FwdSplitCfg<W, 4>;
+  auto kernel = mha_prefix_short_kernel<T, W>;
+  static std::atomic<uint64_t> ready{0};
+  const int attr = ensure_smem(kernel, C::SMEM, ready);
+  if (attr != SPARK_OK) return attr;
+  const int nqt = (p.Nq * (p.H / p.Hkv) + 31) / 32;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(256), C::SMEM, st, p, static_cast<T*>(O), LSE, nqt,
+                     scale * 1.4426950408889634f);
+  return launch_ok("forward kernel (prefix, few keys)") ? SPARK_OK : SPARK_ERR_LAUNCH;
+}
+
 template <typename T>
 int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, void* workspace, float scale, hipStream_t st) {
+  if (prefix_short(p))
+    return p.dh <= 64 ? launch_prefix_short<T, 64>(p, O, LSE, scale, st) : launch_prefix_short<T, 128>(p, O, LSE, scale, st);
   if (workspace && prefix_packed(p)) {
     if (p.dh <= 64) return launch_prefix_parts<T, 64>(p, O, LSE, workspace, scale, st);
     if (p.dh <= 96) return launch_prefix_parts<T, 96>(p, O, LSE, workspace, scale, st);

@@ -125,6 +125,29 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_parts_kernel(PrefixProblem 
                                                  scale_log2, Dropout{}, 1, nullptr, rows);
 }
 
+// Few keys and few rows: a workgroup takes all keys of 32 packed rows of one sequence, its four waves a stream each
+// (fwd_split_tiles), and nothing is merged afterwards.
+template <typename T, int W>
+__global__ __launch_bounds__(256, 2) void mha_prefix_short_kernel(PrefixProblem p, T* __restrict__ O, float* __restrict__ LSE, int nqt,
+                                                                  float scale_log2) {
+  const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int flat = logical / nqt, item = logical - flat * nqt;
+  const PrefixHead x(p, flat);
+  const PrefixAndSuffix<T> keys = keys_of<T>(p, x, item);
+  const int h0 = x.hk * keys.per, all = p.Nq * keys.per;
+  O += (size_t)x.b * (size_t)p.mo.batch + (size_t)h0 * (size_t)p.mo.head;
+  LSE += ((size_t)x.b * p.H + h0) * (size_t)p.Nq;
+  const int row0 = item * 32, row1 = row0 + 32 < all ? row0 + 32 : all;
+  if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
+    zero_rows(O, p.mo, keys, row0, row1, p.dh);
+    for (int r = row0 + threadIdx.x; r < row1; r += 256) LSE[keys.stat(r)] = -INFINITY;
+    return;
+  }
+  fwd_split_tiles<T, W, false, false, false, 4>(head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk),
+                                                head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, LSE, p.mq, p.mks, p.mvs, p.mo, p.H, all,
+                                                x.S, p.dh, nqt, 0, scale_log2, Dropout{}, 1, nullptr, keys);
+}
+
 // A row's parts: W / 4 lanes to a part, SIDE of them side by side, four requested together by each; as many rows to a
 // workgroup as then fit.
 template <typename T, int W, int SIDE>

@@ -80,6 +80,17 @@ def test_ragged_lengths_and_empty_rows(d, dtype, causal):
     check(1, 6, 4, 2, 150, 257, 200, d, dtype, causal, sl=sl, ql=[0, 0, 0, 0, 0, 0], seed=4)
 
 
+@pytest.mark.parametrize("G, B, H, Hkv, N, P, d, dtype", [(2, 44, 16, 16, 20, 150, 64, F16), (1, 16, 16, 16, 40, 200, 128, BF16),
+                                                          (5, 20, 32, 16, 33, 130, 80, BF16), (1, 70, 8, 8, 3, 900, 48, BF16),
+                                                          (2, 28, 24, 8, 50, 0, 112, F16)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_a_grid_for_each_side(G, B, H, Hkv, N, P, d, dtype, causal):
+    """Enough tiles of queries for dQ to have a grid of its own."""
+    check(G, B, H, Hkv, N, P, N, d, dtype, causal, seed=15)
+    sl = [(7 * b) % (N + 1) for b in range(B)]
+    check(G, B, H, Hkv, N, P, N, d, dtype, causal, pl=[P - g for g in range(G)], sl=sl, ql=sl[::-1], seed=15)
+
+
 @pytest.mark.parametrize("d", [64, 80, 128])
 def test_slices_of_packed_projections(d):
     check(2, 4, 6, 2, 150, 200, 150, d, BF16, layout="packed", seed=6)

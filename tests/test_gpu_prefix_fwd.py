@@ -67,38 +67,57 @@ def check(G, B, H, Hkv, Nq, P, S, d, dtype, causal=True, pl=None, ql=None, sl=No
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("d", [8, 40, 64, 72, 96, 104, 128])
 @pytest.mark.parametrize("causal", [False, True])
-def test_head_sizes(d, causal, dtype):
-    check(1, 2, 4, 2, 70, 131, 70, d, dtype, causal)
+@pytest.mark.parametrize("more", [0, 704])  # few keys are one kernel's, more of them others'
+def test_head_sizes(d, causal, dtype, more):
+    check(1, 2, 4, 2, 70, 131 + more, 70, d, dtype, causal)
 
 
 @pytest.mark.parametrize("P, S, Nq", [(1, 1, 1), (64, 1, 1), (63, 5, 1), (65, 64, 1), (200, 16, 1), (0, 7, 1), (0, 130, 130),
                                       (5, 0, 3), (128, 0, 200), (1, 257, 257), (300, 300, 129), (64, 100, 300), (2000, 33, 4),
                                       (640, 513, 500), (127, 127, 127), (64, 64, 64), (1000, 3, 257)])
 @pytest.mark.parametrize("causal", [False, True])
-def test_lengths(P, S, Nq, causal):
-    check(1, 3, 2, 2, Nq, P, S, 64, F16, causal, seed=2)
-    check(1, 3, 2, 1, Nq, P, S, 128, BF16, causal, seed=2)
+@pytest.mark.parametrize("more", [0, 704])
+def test_lengths(P, S, Nq, causal, more):
+    check(1, 3, 2, 2, Nq, P + more, S, 64, F16, causal, seed=2)
+    check(1, 3, 2, 1, Nq, P + more, S, 128, BF16, causal, seed=2)
+
+
+def test_long_suffixes():
+    check(2, 4, 3, 3, 1, 30, 1500, 64, F16, seed=2)
+    check(2, 4, 6, 2, 7, 0, 1500, 128, BF16, seed=2, sl=[1500, 7, 0, 1111], ql=[7, 7, 3, 5])
+    check(1, 2, 3, 1, 600, 64, 700, 72, BF16, seed=2, sl=[700, 333], ql=[600, 400])
 
 
 @pytest.mark.parametrize("G, B, H, Hkv, Nq", [(1, 1, 1, 1, 1), (1, 64, 8, 2, 1), (3, 12, 8, 2, 5), (2, 2, 12, 4, 33), (5, 5, 6, 1, 1),
                                              (4, 8, 16, 16, 1), (1, 7, 32, 1, 2), (1, 200, 2, 2, 1)])
-def test_groups_and_shared_heads(G, B, H, Hkv, Nq):
-    check(G, B, H, Hkv, Nq, 333, 77, 64, BF16, seed=3)
-    check(G, B, H, Hkv, Nq, 150, 70, 128, F16, seed=3)
+@pytest.mark.parametrize("more", [0, 704])
+def test_groups_and_shared_heads(G, B, H, Hkv, Nq, more):
+    check(G, B, H, Hkv, Nq, 333 + more, 77, 64, BF16, seed=3)
+    check(G, B, H, Hkv, Nq, 150 + more, 70, 128, F16, seed=3)
 
 
 @pytest.mark.parametrize("d, dtype", [(64, F16), (128, BF16), (80, BF16)])
 @pytest.mark.parametrize("causal", [False, True])
-def test_ragged_lengths_and_empty_rows(d, dtype, causal):
-    pl, sl = [0, 130, 257], [0, 1, 64, 130, 200, 77]
-    check(3, 6, 4, 2, 1, 257, 200, d, dtype, causal, pl=pl, sl=sl, seed=4)
-    check(3, 6, 4, 2, 200, 257, 200, d, dtype, causal, pl=pl, sl=sl, ql=sl, seed=4)
-    check(3, 6, 4, 2, 9, 257, 200, d, dtype, causal, pl=pl, sl=sl, ql=[9, 3, 0, 1, 9, 8], seed=4)
+@pytest.mark.parametrize("P", [257, 961])
+def test_ragged_lengths_and_empty_rows(d, dtype, causal, P):
+    pl, sl = [0, 130, P], [0, 1, 64, 130, 200, 77]
+    check(3, 6, 4, 2, 1, P, 200, d, dtype, causal, pl=pl, sl=sl, seed=4)
+    check(3, 6, 4, 2, 200, P, 200, d, dtype, causal, pl=pl, sl=sl, ql=sl, seed=4)
+    check(3, 6, 6, 2, 9, P, 200, d, dtype, causal, pl=pl, sl=sl, ql=[9, 3, 0, 1, 9, 8], seed=4)
     # more queries than suffix keys: the first rows see the prefix alone, or nothing
-    check(3, 6, 4, 2, 150, 257, 200, d, dtype, causal, pl=pl, sl=sl, ql=[150, 70, 150, 1, 0, 149], seed=4)
+    check(3, 6, 4, 2, 150, P, 200, d, dtype, causal, pl=pl, sl=sl, ql=[150, 70, 150, 1, 0, 149], seed=4)
+    check(3, 6, 15, 3, 20, P, 200, d, dtype, causal, pl=pl, sl=sl, ql=[20, 7, 20, 1, 0, 19], seed=4)
+
+
+@pytest.mark.parametrize("d", [72, 128])
+def test_workgroups_of_eight_waves(d):
+    """Long sequences with more tiles of 128 rows than CUs, and not as many of 256."""
+    check(1, 2, 8, 8, 2100, 100, 2100, d, BF16, seed=14, sl=[2100, 1990], ql=[2100, 1990])
+    check(2, 2, 16, 4, 1050, 1100, 1050, d, F16, False, seed=14, pl=[1100, 1025], sl=[1000, 1050], ql=[1050, 1049])
 
 
 def test_lengths_out_of_range_are_cut():
+    check(2, 4, 2, 2, 5, 900, 40, 64, F16, True, pl=[2 ** 31 - 1, -3], ql=[7, -1, 5, 2 ** 31 - 1], sl=[41, 12, -2 ** 31, 1000], seed=5)
     check(2, 4, 2, 2, 5, 100, 40, 64, F16, True, pl=[2 ** 31 - 1, -3], ql=[7, -1, 5, 2 ** 31 - 1], sl=[41, 12, -2 ** 31, 1000], seed=5)
 
 
