@@ -649,10 +649,10 @@ static __device__ __forceinline__ void bwd_dq(
       if constexpr (!STATS)
         load_row_frags(of, BufView(Oh, head_span_bytes(mo, Nq, dh)), (uint32_t)qrow_c * ((uint32_t)mo.row * 2), g, dh);
     }
-    size_t stat = (size_t)head * Nq + qrow_c;  // this row's place in the statistics
-    if constexpr (Keys::PREFIX) stat = keys.stat(qrow_c);
-    float lse2 = STATS ? LSE2ws[stat] : LSE[stat];
-    float Dq = STATS ? -Dws[stat] : 0.f;
+    if constexpr (Keys::PREFIX) LSE += keys.stat(qrow_c), LSE2ws += keys.stat(qrow_c), Dws += keys.stat(qrow_c);
+    float lse2 = Keys::PREFIX ? (STATS ? *LSE2ws : *LSE)
+                              : STATS ? LSE2ws[(size_t)head * Nq + qrow_c] : LSE[(size_t)head * Nq + qrow_c];
+    float Dq = !STATS ? 0.f : Keys::PREFIX ? -*Dws : -Dws[(size_t)head * Nq + qrow_c];
 
     int kv_end = Nk;
     if constexpr (Keys::PREFIX) {
@@ -692,10 +692,15 @@ static __device__ __forceinline__ void bwd_dq(
         for (int i = 0; i < 8; ++i) Dq = __builtin_fmaf((float)of[ks][i], (float)dof[ks][i], Dq);
       Dq = half_pair_sum(Dq) * (DROP ? dr.keep_prob : 1.0f);
       lse2 *= 1.4426950408889634f;
-      if (Keys::PREFIX && lse2 == -INFINITY) lse2 = INFINITY;  // a row without keys: P = exp2(s - inf) = 0
-      if (g == 0 && qrow < q_end && (!Keys::PREFIX || keys.part == 0)) {
-        Dws[stat] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
-        LSE2ws[stat] = lse2;
+      if constexpr (Keys::PREFIX) {
+        if (lse2 == -INFINITY) lse2 = INFINITY;  // a row without keys: P = exp2(s - inf) = 0
+        if (g == 0 && qrow < q_end && keys.part == 0) {
+          *Dws = -Dq;
+          *LSE2ws = lse2;
+        }
+      } else if (g == 0 && qrow < Nq) {
+        Dws[(size_t)head * Nq + qrow] = -Dq;  // negated: the dK/dV kernel starts its dP accumulators from it
+        LSE2ws[(size_t)head * Nq + qrow] = lse2;
       }
     }
 #pragma unroll
