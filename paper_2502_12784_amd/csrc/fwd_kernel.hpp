@@ -75,7 +75,7 @@ struct OneSequence {
 // The query rows of the `per` heads that share the keys are packed: row r is query r / per of head r % per (Q, O, LSE: of
 // the first of these heads; Nq: all packed rows).  Neighbouring rows then see nearly the same keys, and only the last of the
 // sequence's tiles is partly empty, not one of every head (us, 16 sequences of 257 to 512 queries behind 1024 keys, 16 heads
-// over 4, forward 86.1 -> FWDUS, dQ 118.5 -> DQUS).
+// over 4, forward 86.1 -> 81.8, dQ 118.5 -> 112.8).
 template <typename T> struct PrefixAndSuffix {
   static constexpr bool PREFIX = true, PACKED = false;
   static constexpr int head = 0, seen = 0;  // not used

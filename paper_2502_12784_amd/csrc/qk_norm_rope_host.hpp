@@ -35,11 +35,14 @@ int qk_vec(int d, int rd) { return d % 16 == 0 && rd % 16 == 0 ? 8 : 4; }
 // Lanes of a row: 4 rows' widths of 64 and 128 columns.
 int qk_lanes(int d, int vec) { return (d <= 64 ? 64 : 128) / (2 * vec); }
 
-// Heads of a workgroup: as many as leave two workgroups to a CU.  (us, at least 1024 -> 512 workgroups: a step of 3 x 1333
-// tokens, 16 heads of 80 30.2 -> 23.5, 16384 x 40 heads of 64 83.9 -> 83.0, a forward of 8192 x 32 of 128 26.8 -> 27.8.)
-int qk_group(const QkNormRope& a, int token_blocks) {
+// Heads of a workgroup: as many as leave three workgroups to a CU, in the backward, whose rows are twice as many, one and a half.
+// (us, at least 512 / 768 / 960 / 1500 workgroups: forward 8192 x 32 heads of 128 28.2 / 27.4 / 27.6 / 30.3, 3 x 1333 x 16 of 80 8.2 /
+// 8.2 / 8.1 / 10.5; steps with 256 / 384 / 512 / 960 in the backward: 3 x 1333 x 16 of 80 22.1 / 20.6 / 22.8 / 26.3, 4096 x 40 of 128
+// 48.1 / 47.5 / 49.4 / 52.9, 16384 x 40 of 64 83.6 / 82.4 / 82.4 / 87.4.)
+int qk_group(const QkNormRope& a, int token_blocks, bool backward) {
+  const int least = backward ? 384 : 768;
   int group = 16;
-  while (group > 1 && (int64_t)token_blocks * ((a.H + group - 1) / group + (a.Hkv + group - 1) / group) < 512) group /= 2;
+  while (group > 1 && (int64_t)token_blocks * ((a.H + group - 1) / group + (a.Hkv + group - 1) / group) < least) group /= 2;
   return group;
 }
 
@@ -49,7 +52,7 @@ struct QkGrid {
 QkGrid qk_grid(QkNormRope* a, bool backward) {
   const int vec = qk_vec(a->d, a->rd), slots = 256 / qk_lanes(a->d, vec);
   const int token_blocks = (int)(((int64_t)a->tokens + slots - 1) / slots);
-  a->group = qk_group(*a, token_blocks);
+  a->group = qk_group(*a, token_blocks, backward);
   a->q_groups = (a->H + a->group - 1) / a->group;
   const int y = a->q_groups + (a->Hkv + a->group - 1) / a->group;
   if (!backward) return QkGrid{token_blocks, y};
