@@ -83,8 +83,8 @@ bool prefix_packed(const PrefixProblem& p) {
   return filled < (p.P <= 1280 ? 48 : 60);
 }
 // The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
-// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's places; a prefix that is only
-// read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256
+// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's places; a
+// prefix that is only read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256
 // workgroups 23.1 / 23.0 / 23.8 / 25.6 / 25.9; 96 suffixes, 4001 keys 23.4 / 23.8 / 23.5 / 16.7 / 16.1; 256 rows, 16384 keys,
 // 128 / 256 / 384 / 512 58 / 51 / 55 / 63).
 PrefixParts prefix_runs(const PrefixProblem& p) {
@@ -95,16 +95,18 @@ PrefixParts prefix_runs(const PrefixProblem& p) {
   s.p_tiles = p.P ? (int)((rows + (s.wide ? 127 : 31)) / (s.wide ? 128 : 32)) : 0;
   s.s_tiles = p.S ? (int)((p.Nq * per + 31) / 32) : 0;
   const int64_t n1 = (int64_t)p.G * p.Hkv * s.p_tiles, n2 = (int64_t)p.B * p.Hkv * s.s_tiles;
-  auto runs = [](int64_t places, int64_t items, int64_t units, int64_t most) {
+  // 64 runs at most (16 instead, of one sequence's suffix alone, d = 128, 8 heads over 1, 65536 keys 32.7 us, so 16.3; 32 over 8,
+  // 131072 keys 107.6, 97.5)
+  auto runs = [](int64_t places, int64_t items, int64_t units) {
     int64_t n = items ? places / items : 0;
     if (n > units) n = units;
-    if (n > most) n = most;
+    if (n > 64) n = 64;
     return (int)(n < 1 ? 1 : n);
   };
   const int64_t places = s.wide || n2 <= 256 ? 256 : n2 >= 416 ? 96 : 512 - n2;
   // at least four tiles of the wide loop to a run, or two rounds of the four key streams
-  s.p_parts = p.P ? runs(places, n1, s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn), 64) : 0;
-  s.s_parts = p.S ? runs(256, n2, (p.S + 8 * bn - 1) / (8 * bn), 16) : 0;
+  s.p_parts = p.P ? runs(places, n1, s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn)) : 0;
+  s.s_parts = p.S ? runs(256, n2, (p.S + 8 * bn - 1) / (8 * bn)) : 0;
   s.p_items = (int)(n1 * s.p_parts);
   return s;
 }

@@ -88,6 +88,12 @@ def test_long_suffixes():
     check(1, 2, 3, 1, 600, 64, 700, 72, BF16, seed=2, sl=[700, 333], ql=[600, 400])
 
 
+def test_many_runs_of_keys():
+    check(1, 1, 4, 1, 1, 0, 20000, 128, BF16, seed=16)
+    check(1, 2, 4, 2, 3, 9000, 9000, 64, F16, seed=16, sl=[9000, 12], ql=[3, 1])
+    check(1, 1, 2, 2, 2, 19000, 5, 40, F16, seed=16, pl=[18111])
+
+
 @pytest.mark.parametrize("G, B, H, Hkv, Nq", [(1, 1, 1, 1, 1), (1, 64, 8, 2, 1), (3, 12, 8, 2, 5), (2, 2, 12, 4, 33), (5, 5, 6, 1, 1),
                                              (4, 8, 16, 16, 1), (1, 7, 32, 1, 2), (1, 200, 2, 2, 1)])
 @pytest.mark.parametrize("more", [0, 704])
