@@ -57,18 +57,6 @@ bool prefix_wide(const PrefixProblem& p) {
   return (int64_t)p.P + p.S >= 2048 && 7 * wide <= 4 * narrow && (wide >= 512 || narrow >= 896 || (wide <= 256 && narrow > 256));
 }
 
-// Whether 32 packed rows of a sequence go to a workgroup with all their keys (mha_prefix_short_kernel): up to four rounds of its
-// key streams, while the workgroups are resident together or a sequence's rows fit one.  Forward, us, otherwise / so, sequences x
-// heads x queries behind P + S keys:
-//   d = 128:  32 x 16 x 1 behind 64 + 64 9.9 / 9.7, 256 + 64 13.9 / 11.8, 384 + 64 14.0 / 13.2, 640 + 64 14.4 / 16.1
-//             8 x 16 x 16 behind 256 + 64 12.8 / 8.8, 512 + 64 13.8 / 11.0, 1024 + 64 15.5 / 16.3     8 x 16 x 64 behind 128 + 64 9.2 / 8.5
-//             4 x 32 over 8 x 1 behind 128 + 200 9.4 / 8.6, 512 + 200 9.8 / 11.8     64 x 32 over 8 x 1 behind 128 + 100 17.2 / 11.4
-//   d = 64:   2 x 4 x 1 behind 64 + 20 6.3 / 5.6, 512 + 20 8.3 / 8.1, 1024 + 20 8.4 / 10.3     1 x 8 x 100 behind 100 + 100 8.5 / 6.1
-bool prefix_short(const PrefixProblem& p) {
-  const int64_t tiles = ((int64_t)p.Nq * (p.H / p.Hkv) + 31) / 32;
-  return (int64_t)p.P + p.S <= (p.dh <= 64 ? 640 : 512) && (tiles == 1 || p.B * (int64_t)p.Hkv * tiles <= 512);
-}
-
 // Whether rows are packed across sequences and the keys go to several workgroups in runs (prefix_parts.hpp), or every tile of a
 // sequence's rows walks all its keys by itself: where those tiles fill the chip and are well filled themselves.  Forward, us,
 // d = 128 but where said, packed / by themselves:
@@ -82,6 +70,34 @@ bool prefix_packed(const PrefixProblem& p) {
   const int64_t filled = 100 * rows / (128 * tiles);  // percent of the tiles' rows
   return filled < (p.P <= 1280 ? 48 : 60);
 }
+
+// Whether 32 packed rows of a sequence go to a workgroup with all their keys (mha_prefix_short_kernel, two to a CU): a chain of
+// keys / 128 rounds (at 64 columns / 256) and no merge, against runs of keys and a merge (prefix_packed).  Forward, us, otherwise /
+// so.  Where a sequence's rows fit one workgroup, packing reads the prefix for many sequences at once, and few keys are the limit
+// (sequences x heads x queries behind P + S keys):
+//   d = 128:  32 x 16 x 1 behind 64 + 64 9.9 / 9.7, 256 + 64 13.9 / 11.8, 384 + 64 14.0 / 13.2, 640 + 64 14.4 / 16.1
+//             8 x 16 x 16 behind 256 + 64 12.8 / 8.8, 512 + 64 13.8 / 11.0, 1024 + 64 15.5 / 16.3
+//             4 x 32 over 8 x 1 behind 128 + 200 9.4 / 8.6, 512 + 200 9.8 / 11.8     64 x 32 over 8 x 1 behind 128 + 100 17.2 / 11.4
+//   d = 64:   2 x 4 x 1 behind 64 + 20 6.3 / 5.6, 512 + 20 8.3 / 8.1, 1024 + 20 8.4 / 10.3
+// With more rows, the more workgroups the more keys, as runs are fewer then (n workgroups, keys):
+//   d = 128:  64: 1088 15.2 / 15.1, 2112 18.4 / 23.2      128: 1088 19.1 / 16.0, 2112 24.1 / 24.5    256: 1152 24.8 / 16.3, 2112 24.9 / 25.1,
+//             4224 35.8 / 41.8    512: 1274 30.7 / 23.8, 2298 37.3 / 36.8, 4346 53.5 / 60.6            768: 576 29.5 / 24.7, 1088 33.6 / 33.9
+//   d = 64:   64: 1280 10.9 / 10.6, 2112 12.9 / 15.4      128: 1088 13.1 / 10.8, 2112 17.2 / 15.6      256: 1152 17.8 / 11.0, 4128 24.9 / 25.2
+//             512: 1274 23.5 / 15.5, 2298 26.0 / 22.2, 4346 34.6 / 34.6                                768: 1088 24.9 / 22.7, 2112 33.9 / 33.8
+//   against tiles of 128 rows by themselves (1024 workgroups so) 576 keys d = 128 17.5 / 28.0, d = 64 13.1 / 19.7.
+bool prefix_short(const PrefixProblem& p) {
+  const int64_t tiles = ((int64_t)p.Nq * (p.H / p.Hkv) + 31) / 32, groups = p.B * (int64_t)p.Hkv * tiles;
+  const bool narrow = p.dh <= 64;
+  int64_t keys = narrow ? 640 : 512;
+  if (tiles > 1) {
+    if (groups > 768 || (groups > 512 && !prefix_packed(p))) return false;
+    const int64_t most = groups > 512 ? (narrow ? 2048 : 1024) : narrow ? 3200 : 2048;
+    keys += (narrow ? 10 : 8) * groups;
+    if (keys > most) keys = most;
+  }
+  return (int64_t)p.P + p.S <= keys;
+}
+
 // The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
 // that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's places; a
 // prefix that is only read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256

@@ -104,7 +104,7 @@ def test_groups_and_shared_heads(G, B, H, Hkv, Nq, more):
 
 @pytest.mark.parametrize("d, dtype", [(64, F16), (128, BF16), (80, BF16)])
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("P", [257, 961])
+@pytest.mark.parametrize("P", [257, 961, 2300])  # a kernel for few keys, and others
 def test_ragged_lengths_and_empty_rows(d, dtype, causal, P):
     pl, sl = [0, 130, P], [0, 1, 64, 130, 200, 77]
     check(3, 6, 4, 2, 1, P, 200, d, dtype, causal, pl=pl, sl=sl, seed=4)
