@@ -71,31 +71,42 @@ bool prefix_packed(const PrefixProblem& p) {
   return filled < (p.P <= 1280 ? 48 : 60);
 }
 
-// Whether 32 packed rows of a sequence go to a workgroup with all their keys (mha_prefix_short_kernel, two to a CU): a chain of
-// keys / 128 rounds (at 64 columns / 256) and no merge, against runs of keys and a merge (prefix_packed).  Forward, us, otherwise /
-// so.  Where a sequence's rows fit one workgroup, packing reads the prefix for many sequences at once, and few keys are the limit
-// (sequences x heads x queries behind P + S keys):
-//   d = 128:  32 x 16 x 1 behind 64 + 64 9.9 / 9.7, 256 + 64 13.9 / 11.8, 384 + 64 14.0 / 13.2, 640 + 64 14.4 / 16.1
-//             8 x 16 x 16 behind 256 + 64 12.8 / 8.8, 512 + 64 13.8 / 11.0, 1024 + 64 15.5 / 16.3
-//             4 x 32 over 8 x 1 behind 128 + 200 9.4 / 8.6, 512 + 200 9.8 / 11.8     64 x 32 over 8 x 1 behind 128 + 100 17.2 / 11.4
-//   d = 64:   2 x 4 x 1 behind 64 + 20 6.3 / 5.6, 512 + 20 8.3 / 8.1, 1024 + 20 8.4 / 10.3
-// With more rows, the more workgroups the more keys, as runs are fewer then (n workgroups, keys):
-//   d = 128:  64: 1088 15.2 / 15.1, 2112 18.4 / 23.2      128: 1088 19.1 / 16.0, 2112 24.1 / 24.5    256: 1152 24.8 / 16.3, 2112 24.9 / 25.1,
-//             4224 35.8 / 41.8    512: 1274 30.7 / 23.8, 2298 37.3 / 36.8, 4346 53.5 / 60.6            768: 576 29.5 / 24.7, 1088 33.6 / 33.9
-//   d = 64:   64: 1280 10.9 / 10.6, 2112 12.9 / 15.4      128: 1088 13.1 / 10.8, 2112 17.2 / 15.6      256: 1152 17.8 / 11.0, 4128 24.9 / 25.2
-//             512: 1274 23.5 / 15.5, 2298 26.0 / 22.2, 4346 34.6 / 34.6                                768: 1088 24.9 / 22.7, 2112 33.9 / 33.8
-//   against tiles of 128 rows by themselves (1024 workgroups so) 576 keys d = 128 17.5 / 28.0, d = 64 13.1 / 19.7.
-bool prefix_short(const PrefixProblem& p) {
-  const int64_t tiles = ((int64_t)p.Nq * (p.H / p.Hkv) + 31) / 32, groups = p.B * (int64_t)p.Hkv * tiles;
+// Whether 32 packed rows of a sequence go to a workgroup with all their keys (mha_prefix_short_kernel): a chain of keys / 256 rounds
+// (at 64 columns / 512; of four waves instead of eight, half of that) and no merge, against runs of keys and a merge
+// (prefix_packed).  Returns its waves: eight up to one workgroup per CU, four, two workgroups to a CU, for more of them or few
+// keys; 0: not so.  Forward, us, in runs / so (n workgroups, keys):
+//   d = 128:  56: 1088 13.6 / 12.9, 2112 16.9 / 18.0    64: 2112 19.0 / 17.9, 4160 24.4 / 28.1   128: 1088 16.6 / 14.6, 2112 20.1 / 20.3
+//             256: 1088 16.1 / 14.1, 2112 27.8 / 20.4, or 23.0 / 21.5 at 40 rows a sequence, then 4160 30.3 / 35.0
+//             512: 1274 30.7 / 23.8, 2298 37.3 / 36.8, 4346 53.5 / 60.6              768: 576 29.5 / 24.7, 1088 33.6 / 33.9
+//   d = 64:   56: 1088 10.6 / 9.6, 2112 12.0 / 12.2     64: 2112 13.0 / 12.5, 4160 18.8 / 17.9   128: 2112 14.4 / 13.7, 4160 18.3 / 19.5
+//             256: 2112 16.8 / 13.4, 4160 25.5 / 19.7, or 21.4 / 21.9 at 40 rows
+//             512: 1274 23.5 / 15.5, 2298 26.0 / 22.2, 4346 34.6 / 34.6              768: 1088 24.9 / 22.7, 2112 33.9 / 33.8
+//   against tiles of 128 rows by themselves (1024 workgroups so) 576 keys d = 128 17.5 / 28.0, d = 64 13.1 / 19.7;
+//   four waves / eight: 64 workgroups d = 64 264 keys 7.2 / 7.5, 564 8.4 / 8.3, 2112 15.3 / 12.5, d = 128 264 9.0 / 9.3, 2112 23.9 / 17.9.
+// Where a sequence's rows fill a part of one workgroup only, packing reads the prefix once for several sequences, and the limit falls
+// with the rows (sequences x heads x queries, keys):
+//   d = 128:  32 x 16 x 1 320 13.9 / 11.8, 448 14.0 / 13.2, 704 14.4 / 16.1; 32 x 16 over 8 x 1 564 11.3 / 10.7, 1088 11.9 / 13.8;
+//             8 x 16 x 16 1088 15.5 / 13.5, 2112 18.7 / 18.8; 4 x 32 over 8 x 1 328 9.4 / 8.6, 712 9.8 / 11.8
+//   d = 64:   2 x 4 x 1 564 8.1 / 8.0, 1088 8.6 / 9.4; 32 x 16 over 8 x 1 564 8.6 / 8.5, 1088 9.3 / 10.0; 8 x 16 x 16 2112 13.3 / 12.5
+int prefix_short(const PrefixProblem& p) {
+  const int64_t rows = (int64_t)p.Nq * (p.H / p.Hkv), tiles = (rows + 31) / 32, groups = p.B * (int64_t)p.Hkv * tiles;
+  const int64_t n = (int64_t)p.P + p.S;
   const bool narrow = p.dh <= 64;
-  int64_t keys = narrow ? 640 : 512;
-  if (tiles > 1) {
-    if (groups > 768 || (groups > 512 && !prefix_packed(p))) return false;
-    const int64_t most = groups > 512 ? (narrow ? 2048 : 1024) : narrow ? 3200 : 2048;
-    keys += (narrow ? 10 : 8) * groups;
-    if (keys > most) keys = most;
+  const int64_t few = narrow ? 640 : 512;
+  int64_t most = few;  // keys
+  if (groups <= 256) {
+    const int64_t line = narrow ? 384 + 32 * groups : 256 + 24 * groups, top = narrow ? 4096 : 2400;
+    most = line < top ? line : top;
+  } else if (groups <= 512) {
+    most = narrow ? 3200 : 2048;
+  } else if (groups <= 768 && prefix_packed(p)) {
+    most = narrow ? 2048 : 1024;
+  } else if (tiles > 1) {
+    return 0;
   }
-  return (int64_t)p.P + p.S <= keys;
+  if (most < few) most = few;
+  if (tiles == 1) most = few + (most - few) * rows / 32;
+  return n > most ? 0 : groups <= 256 && n > 512 ? 8 : 4;
 }
 
 // The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
@@ -158,23 +169,26 @@ int launch_prefix_parts(const PrefixProblem& p, void* O, float* LSE, void* works
   return launch_ok("forward merge kernel (prefix)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
-template <typename T, int W>
+template <typename T, int W, int NW>
 int launch_prefix_short(const PrefixProblem& p, void* O, float* LSE, float scale, hipStream_t st) {
-  using C = FwdSplitCfg<W, 4>;
-  auto kernel = mha_prefix_short_kernel<T, W>;
+  using C = FwdSplitCfg<W, NW>;
+  auto kernel = mha_prefix_short_kernel<T, W, NW>;
   static std::atomic<uint64_t> ready{0};
   const int attr = ensure_smem(kernel, C::SMEM, ready);
   if (attr != SPARK_OK) return attr;
   const int nqt = (p.Nq * (p.H / p.Hkv) + 31) / 32;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(256), C::SMEM, st, p, static_cast<T*>(O), LSE, nqt,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(p.B * p.Hkv * nqt)), dim3(64 * NW), C::SMEM, st, p, static_cast<T*>(O), LSE, nqt,
                      scale * 1.4426950408889634f);
   return launch_ok("forward kernel (prefix, few keys)") ? SPARK_OK : SPARK_ERR_LAUNCH;
 }
 
 template <typename T>
 int dispatch_prefix_fwd(const PrefixProblem& p, void* O, float* LSE, void* workspace, float scale, hipStream_t st) {
-  if (prefix_short(p))
-    return p.dh <= 64 ? launch_prefix_short<T, 64>(p, O, LSE, scale, st) : launch_prefix_short<T, 128>(p, O, LSE, scale, st);
+  const int waves = prefix_short(p);
+  if (waves == 8)
+    return p.dh <= 64 ? launch_prefix_short<T, 64, 8>(p, O, LSE, scale, st) : launch_prefix_short<T, 128, 8>(p, O, LSE, scale, st);
+  if (waves)
+    return p.dh <= 64 ? launch_prefix_short<T, 64, 4>(p, O, LSE, scale, st) : launch_prefix_short<T, 128, 4>(p, O, LSE, scale, st);
   if (workspace && prefix_packed(p)) {
     if (p.dh <= 64) return launch_prefix_parts<T, 64>(p, O, LSE, workspace, scale, st);
     if (p.dh <= 96) return launch_prefix_parts<T, 96>(p, O, LSE, workspace, scale, st);

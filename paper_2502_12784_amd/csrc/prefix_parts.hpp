@@ -125,11 +125,11 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_parts_kernel(PrefixProblem 
                                                  scale_log2, Dropout{}, 1, nullptr, rows);
 }
 
-// Few keys and few rows: a workgroup takes all keys of 32 packed rows of one sequence, its four waves a stream each
+// Few keys and few rows: a workgroup takes all keys of 32 packed rows of one sequence, its waves a stream each
 // (fwd_split_tiles), and nothing is merged afterwards.
-template <typename T, int W>
-__global__ __launch_bounds__(256, 2) void mha_prefix_short_kernel(PrefixProblem p, T* __restrict__ O, float* __restrict__ LSE, int nqt,
-                                                                  float scale_log2) {
+template <typename T, int W, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void mha_prefix_short_kernel(PrefixProblem p, T* __restrict__ O,
+                                                                                    float* __restrict__ LSE, int nqt, float scale_log2) {
   const int logical = xcd_contiguous(blockIdx.x, gridDim.x);
   const int flat = logical / nqt, item = logical - flat * nqt;
   const PrefixHead x(p, flat);
@@ -140,10 +140,10 @@ __global__ __launch_bounds__(256, 2) void mha_prefix_short_kernel(PrefixProblem 
   const int row0 = item * 32, row1 = row0 + 32 < all ? row0 + 32 : all;
   if (row0 >= keys.rows || (x.P == 0 && (x.S == 0 || (row1 - 1) / keys.per + x.ahead < 0))) {  // no row in use, or no key for any
     zero_rows(O, p.mo, keys, row0, row1, p.dh);
-    for (int r = row0 + threadIdx.x; r < row1; r += 256) LSE[keys.stat(r)] = -INFINITY;
+    for (int r = row0 + threadIdx.x; r < row1; r += 64 * NW) LSE[keys.stat(r)] = -INFINITY;
     return;
   }
-  fwd_split_tiles<T, W, false, false, false, 4>(head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk),
+  fwd_split_tiles<T, W, false, false, false, NW>(head_of<T>(p.Q, p.mq, x.b, h0), head_of<T>(p.Ks, p.mks, x.b, x.hk),
                                                 head_of<T>(p.Vs, p.mvs, x.b, x.hk), O, LSE, p.mq, p.mks, p.mvs, p.mo, p.H, all,
                                                 x.S, p.dh, nqt, 0, scale_log2, Dropout{}, 1, nullptr, keys);
 }

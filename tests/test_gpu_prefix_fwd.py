@@ -67,7 +67,7 @@ def check(G, B, H, Hkv, Nq, P, S, d, dtype, causal=True, pl=None, ql=None, sl=No
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("d", [8, 40, 64, 72, 96, 104, 128])
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("more", [0, 704])  # few keys are one kernel's, more of them others'
+@pytest.mark.parametrize("more", [0, 704, 2600])  # few keys are one kernel's, more of them others'
 def test_head_sizes(d, causal, dtype, more):
     check(1, 2, 4, 2, 70, 131 + more, 70, d, dtype, causal)
 
@@ -76,7 +76,7 @@ def test_head_sizes(d, causal, dtype, more):
                                       (5, 0, 3), (128, 0, 200), (1, 257, 257), (300, 300, 129), (64, 100, 300), (2000, 33, 4),
                                       (640, 513, 500), (127, 127, 127), (64, 64, 64), (1000, 3, 257)])
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("more", [0, 704])
+@pytest.mark.parametrize("more", [0, 704, 2600])
 def test_lengths(P, S, Nq, causal, more):
     check(1, 3, 2, 2, Nq, P + more, S, 64, F16, causal, seed=2)
     check(1, 3, 2, 1, Nq, P + more, S, 128, BF16, causal, seed=2)
@@ -96,7 +96,7 @@ def test_many_runs_of_keys():
 
 @pytest.mark.parametrize("G, B, H, Hkv, Nq", [(1, 1, 1, 1, 1), (1, 64, 8, 2, 1), (3, 12, 8, 2, 5), (2, 2, 12, 4, 33), (5, 5, 6, 1, 1),
                                              (4, 8, 16, 16, 1), (1, 7, 32, 1, 2), (1, 200, 2, 2, 1)])
-@pytest.mark.parametrize("more", [0, 704])
+@pytest.mark.parametrize("more", [0, 704, 2600])
 def test_groups_and_shared_heads(G, B, H, Hkv, Nq, more):
     check(G, B, H, Hkv, Nq, 333 + more, 77, 64, BF16, seed=3)
     check(G, B, H, Hkv, Nq, 150 + more, 70, 128, F16, seed=3)
@@ -104,7 +104,7 @@ def test_groups_and_shared_heads(G, B, H, Hkv, Nq, more):
 
 @pytest.mark.parametrize("d, dtype", [(64, F16), (128, BF16), (80, BF16)])
 @pytest.mark.parametrize("causal", [False, True])
-@pytest.mark.parametrize("P", [257, 961, 2300])  # a kernel for few keys, and others
+@pytest.mark.parametrize("P", [257, 961, 4100])  # a kernel for few keys, and others
 def test_ragged_lengths_and_empty_rows(d, dtype, causal, P):
     pl, sl = [0, 130, P], [0, 1, 64, 130, 200, 77]
     check(3, 6, 4, 2, 1, P, 200, d, dtype, causal, pl=pl, sl=sl, seed=4)
