@@ -109,11 +109,17 @@ int prefix_short(const PrefixProblem& p) {
   return n > most ? 0 : groups <= 256 && n > 512 ? 8 : 4;
 }
 
-// The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond
-// that multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's places; a
-// prefix that is only read leaves them to the suffixes where these fill them anyway (32 sequences x 16 heads, 4096 keys, 64 / 96 / 128 / 192 / 256
-// workgroups 23.1 / 23.0 / 23.8 / 25.6 / 25.9; 96 suffixes, 4001 keys 23.4 / 23.8 / 23.5 / 16.7 / 16.1; 256 rows, 16384 keys,
-// 128 / 256 / 384 / 512 58 / 51 / 55 / 63).
+// The runs of keys.  Two workgroups fit a CU, 512 in all.  Up to 96 packed rows the prefix is read by tiles of 32 rows, beyond that
+// multiplied in tiles of 128 (us, 80 rows, 4001 keys, d = 64: 16.4, in one tile of 128 18.4).  Its runs fill half of the chip's
+// places; a prefix that is only read leaves them to the suffixes where these fill them anyway (us, 32 sequences x 16 heads, 4096 keys,
+// 64 / 96 / 128 / 192 / 256 workgroups 23.1 / 23.0 / 23.8 / 25.6 / 25.9; 96 suffixes, 4001 keys 23.4 / 23.8 / 23.5 / 16.7 / 16.1).
+// A prefix that is multiplied leaves some to suffixes with as much work, tiles times keys, as its own (32 heads over 8, us, the
+// ratio of the work in front, d = 64 and 128, 128 / 192 / 224 / 256 workgroups; more of them are slower everywhere):
+//   0.1   32 x 5 behind 16384 + 300    65.7 / 52.1 / 45.2 / 41.8     93.6 / 76.1 / 68.8 / 67.3
+//   0.6   48 x 1 behind 8192 + 200     20.8 / 18.3 / 19.8 / 21.7     28.5 / 26.3 / 27.3 / 28.8
+//   1     128 x 1 behind 8192 + 256    33.3 / 31.1 / 32.0 / 33.5     53.2 / 49.2 / 50.4 / 53.0
+//   1     64 x 1 behind 16384 + 512    35.2 / 31.2 / 29.2 / 31.6     56.6 / 50.2 / 48.6 / 49.5
+//   4     128 x 1 behind 8192 + 1024   54.0 / 56.6 / 56.9 / 57.5     94.5 / 98.2 / 98.0 / 101.7
 PrefixParts prefix_runs(const PrefixProblem& p) {
   PrefixParts s{};
   const int64_t per = p.H / p.Hkv, rows = (int64_t)(p.B / p.G) * p.Nq * per;
@@ -130,7 +136,9 @@ PrefixParts prefix_runs(const PrefixProblem& p) {
     if (n > 64) n = 64;
     return (int)(n < 1 ? 1 : n);
   };
-  const int64_t places = s.wide || n2 <= 256 ? 256 : n2 >= 416 ? 96 : 512 - n2;
+  const int64_t p_work = n1 * p.P, s_work = n2 * p.S;
+  const int64_t beside = 5 * s_work < 2 * p_work ? 256 : s_work < 2 * p_work ? 208 : 128;
+  const int64_t places = s.wide ? beside : n2 <= 256 ? 256 : n2 >= 416 ? 96 : 512 - n2;
   // at least four tiles of the wide loop to a run, or two rounds of the four key streams
   s.p_parts = p.P ? runs(places, n1, s.wide ? (p.P + 255) / 256 : (p.P + 8 * bn - 1) / (8 * bn)) : 0;
   s.s_parts = p.S ? runs(256, n2, (p.S + 8 * bn - 1) / (8 * bn)) : 0;
