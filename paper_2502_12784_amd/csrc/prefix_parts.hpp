@@ -14,7 +14,7 @@
 //
 // Bound by memory, and for the smaller ones by the latency of two kernels.  Measured, one new token, d = 128, bf16: 32 sequences x 16
 // heads behind 4096 + up to 256 keys 18.6 us (4.6 TB/s; a read of 1 GiB reaches 4.0, a copy 5.0) and 4.0 for the merge; 64 x 32 heads over 8 behind
-// 16384 + up to 512 35.3 (4.8 TB/s, and 17.6 GFLOP) and 6.3.
+// 16384 + up to 512 35.5 (4.7 TB/s, and 17.6 GFLOP) and 5.6.
 #pragma once
 #include "fwd_split_kernel.hpp"
 #include "prefix_kernels.hpp"
