@@ -375,7 +375,8 @@ int spark_qk_norm_rope_bwd(const void* Q, const void* K, const void* wq, const v
  *               return.  Few query rows per head of keys give too few workgroups unless several share the keys, and the rows
  *               of a group's sequences are packed into common tiles: their partial results are kept there.  May be NULL (and
  *               0 bytes may be all that is needed): same operation, every query tile by one workgroup.  SPARK_ERR_WORKSPACE if it is not
- *               NULL and too small.
+ *               NULL and too small.  The size belongs to these sizes: a smaller problem may be split among more workgroups and need
+ *               more, so a caller that keeps one workspace for several problems takes the largest of their sizes.
  */
 size_t spark_mha_prefix_fwd_workspace_bytes(int G, int B, int H, int Hkv, int Nq, int P, int S, int d, spark_dtype_t dtype);
 

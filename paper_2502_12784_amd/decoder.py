@@ -165,7 +165,8 @@ def spark_mha_prefix_fwd(Q, Kp, Vp, Ks, Vs, scale: float, causal: bool = True, p
     own suffixes Ks, Vs [B,Hkv,S,d].  prefix_lens [G], q_lens, s_lens [B]: int32 on the device, how much of P, Nq, S is in
     use.  causal: query i sees suffix keys j <= i + s_lens - q_lens.  Rows from q_lens on, and rows that see no key, give
     O = 0 and LSE = -inf.  Any strides.  workspace: allocated here if not given; with an empty one every query tile is one
-    workgroup's, which for few rows is slow."""
+    workgroup's, which for few rows is slow; one kept for several problems has the largest of their sizes (a smaller problem
+    may need more)."""
     import torch
     lib = load_library()
     if workspace is None:
